@@ -2,7 +2,8 @@
 
 `binding` marshals arguments into `libcos_verify.so` (every step of the path runs in the
 CUDA kernels; there is no CPU fallback), `synth` makes the seeded synthetic workloads,
-`sharding` splits a batch of rows over ranks.
+`sharding` splits a batch of rows over ranks, `draft` holds the proposer's operators (drawing draft
+tokens, listing a model's largest logits, distillation).
 """
 from .binding import (  # noqa: F401
     COS_COMBINE_LOGIT_LINEAR,
@@ -24,3 +25,4 @@ from .binding import (  # noqa: F401
     CosVerifyError,
     load_library,
 )
+from .draft import COS_TOP_MAX, distill_loss, distill_step, sample, top_logits  # noqa: F401

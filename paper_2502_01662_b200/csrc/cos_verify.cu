@@ -939,6 +939,14 @@ extern "C" const char* cos_verify_last_error(const cos_verify_ctx* ctx) {
   return ctx ? ctx->err.c_str() : g_create_error.c_str();
 }
 
+namespace cosv {
+cos_status call_failed(cos_status st, const char* what) {
+  g_create_error = what;
+  return st;
+}
+cos_status call_failed(const char* what, cudaError_t e) { return cuda_fail(nullptr, what, e); }
+}  // namespace cosv
+
 // ------------------------------------------------------------------------------------
 // verification without a context and without any device allocation
 // ------------------------------------------------------------------------------------

@@ -5,8 +5,8 @@
  * logits (cos_sample), and a proposer learns to have more of its drafts accepted from the
  * largest logits of the models it is verified against (cos_top_logits, cos_distill).
  *
- * All pointers are DEVICE pointers owned by the caller.  Every function enqueues one launch on
- * `cuda_stream`, on the device named in its arguments (the calling thread's current device stays as it
+ * All pointers are DEVICE pointers owned by the caller.  Every function enqueues one launch (two for
+ * cos_distill_loss and cos_distill_step) on `cuda_stream`, on the device named in its arguments (the calling thread's current device stays as it
  * is), allocates nothing, keeps nothing between calls and returns without waiting; calls on any
  * number of streams may overlap, and a call may be captured into a CUDA graph.  Problems the host can
  * see are returned (the reason is in cos_verify_last_error(NULL)) and nothing is enqueued then;
@@ -21,6 +21,7 @@
 extern "C" {
 #endif
 
+#define COS_DISTILL_STATISTICS 8 /* floats of a row beside its lists' shares */
 #define COS_TOP_MAX 1024 /* most entries cos_top_logits lists for a row, and cos_distill takes for one */
 
 typedef struct {
@@ -105,8 +106,8 @@ typedef struct {
   const float* row_weights; /* [rows]: what the loss of each row counts in the sum whose gradient is    */
                           /* wanted; rows of weight 0 have gradient 0 whatever they hold                */
   float* loss;            /* out [rows] */
-  float* statistics;      /* [rows][2], 8-byte aligned: the student's largest logit and log2 of its     */
-                          /* normaliser at T; written by cos_distill_loss, read by cos_distill_grad     */
+  float* statistics;      /* rows * (COS_DISTILL_STATISTICS + lists * k) floats, 16-byte aligned: what  */
+                          /* cos_distill_loss leaves for cos_distill_grad; cos_distill_step's own       */
   void* grad;             /* out [rows][vocab], of the student's type; may be `student` itself with the */
                           /* same stride; must not overlap it otherwise                                 */
   int64_t stride_grad;
@@ -118,8 +119,8 @@ typedef struct {
  *   loss = sum_x t(x) (ln t(x) - ln q(x)),   gradient = row_weight / T * (P q(x) - t(x)),  P = sum_x t(x).
  * +inf where a token with a share has the logit -inf.  A row without a share (padding) has loss 0 and gradient 0 and is not read.
  *   cos_distill_loss  loss and statistics (row_weights, grad are not looked at)
- *   cos_distill_grad  the gradient, from the statistics of the same student, lists and T (loss is not looked at)
- *   cos_distill_step  loss and gradient in one launch that reads the student once (statistics are not looked at)
+ *   cos_distill_grad  the gradient, from the statistics of the same student, lists and T (loss, values and lse are not looked at)
+ *   cos_distill_step  loss and gradient, reading the student once
  */
 cos_status cos_distill_loss(const cos_distill_args* args, void* cuda_stream);
 cos_status cos_distill_grad(const cos_distill_args* args, void* cuda_stream);

@@ -1,24 +1,37 @@
 // Distillation from the largest logits of a row's teachers: the loss, its gradient, and both in one launch.
 //
 // Mathematics.  loss = sum over the listed tokens of t (ln t - s/T) + P lse(s/T), so beside the student's normaliser the loss takes the listed tokens alone
-// (both relative to the student's largest logit);
-// the gradient is P q everywhere, with t taken off at the listed tokens.  Shares of a token that comes up more than once are added by the first of its
-// entries, in order, so results do not depend on timing.
+// (both relative to the student's logit at one of them, so that nothing large is subtracted); the gradient is P q everywhere, with t taken off at the listed
+// tokens.  Shares of a token that comes up more than once are added by the first of its entries, in order, so results do not depend on timing.
 //
-// Bound by memory: the loss reads the student once, the gradient reads it and writes as much; the launch with both keeps a row in the shared memory of a
-// cluster of blocks between the normaliser and the gradient, and reads it once.  Exponentials are 32-bit (2^-22) and sums of them 64-bit; shares, logarithms and
-// the loss are 64-bit; the gradient is rounded once.
+// Two launches for the loss, and for loss and gradient together: the shares (a block for each row looks at its entries; a few microseconds, in which the first rows of the
+// other launch are on their way already), then the rows.  Bound by memory: the loss reads the student once, the gradient reads it and writes as much; the rows of the
+// launch with both stay in the shared memory of a cluster of blocks between the normaliser and the gradient, and are read once.  Three blocks of a multiprocessor
+// have up to 64 KB each under way, since a row's chain of steps (copies, two sweeps, a barrier, the gradient) takes longer than its bytes.
+// Exponentials are 32-bit (2^-22) and sums of them 64-bit; shares, logarithms and the loss are 64-bit; the gradient is rounded once.
 #include <cuda_bf16.h>
+
+#include <type_traits>
 
 #include "cos_slice.cuh"
 
 namespace cosv {
 namespace {
 
+// What a row's launches leave for the next (COS_DISTILL_STATISTICS floats): the student's largest logit and log2 of its normaliser; the sum of the shares; the
+// reference logit, and the sum over the listed tokens of t (ln t - (s - reference) / T).
+struct Statistics {
+  float m, log_z, mass, reference;
+  double listed, mass64;
+};
+static_assert(sizeof(Statistics) == COS_DISTILL_STATISTICS * sizeof(float), "as the header says");
+constexpr int kLoss = 0, kGrad = 1, kStep = 2, kShareThreads = 128;
+
 struct DistillParams {
   const char* student;
   long long stride;
   int rows, V, parts, share, seg, res;
+  int early;  // blocks that may start on their rows before the shares are there
   int lists, k;
   const int* ids;
   const float* values;
@@ -27,18 +40,16 @@ struct DistillParams {
   float T;
   const float* row_weights;
   float* loss;
-  float2* statistics;
+  float* statistics;
   char* grad;
   long long stride_grad;
 };
 
-// The listed tokens of a row that lie in this block's slice, each once.
+// The entries of a row, in shared memory.
 struct Shares {
-  int id[COS_TOP_MAX];
-  double t[COS_TOP_MAX];
-  double warp[kSliceWarps];
-  int bad;
-  double list_max[COS_MAX_MODELS], list_sum[COS_MAX_MODELS];
+  double* t;  // 0 for an empty entry
+  int* id;
+  double *per_warp, *list_max, *list_sum;
 };
 
 __device__ __forceinline__ double warp_sum(double v) {
@@ -51,20 +62,19 @@ __device__ __forceinline__ double block_sum(double v, double* per_warp) {
   if ((threadIdx.x & 31) == 0) per_warp[threadIdx.x >> 5] = v;
   __syncthreads();
   double s = 0.0;
-  for (int w = 0; w < kSliceWarps; ++w) s += per_warp[w];
+  for (int w = 0; w < kShareThreads / 32; ++w) s += per_warp[w];
   __syncthreads();
   return s;
 }
 
 // Every entry's share to shared memory (0 for an empty one); returns their sum, NaN where an entry names no token.
-__device__ __forceinline__ double row_shares(const DistillParams& p, int row, Shares& sh) {
+__device__ __forceinline__ double row_shares(const DistillParams& p, int row, const Shares& sh) {
   const int n = p.lists * p.k, tid = threadIdx.x;
   const int* ids = p.ids + static_cast<long long>(row) * n;
   const float* values = p.values + static_cast<long long>(row) * n;
   const double inv_T = 1.0 / static_cast<double>(p.T);
   if (!p.lse) {  // softmax over each list: a warp for each
-    const int g = tid >> 5;
-    if (g < p.lists) {
+    for (int g = tid >> 5; g < p.lists; g += kShareThreads / 32) {
       double m = -INFINITY, s = 0.0;
       for (int i = tid & 31; i < p.k; i += 32)
         if (ids[g * p.k + i] >= 0) m = fmax(m, static_cast<double>(values[g * p.k + i]));
@@ -81,7 +91,7 @@ __device__ __forceinline__ double row_shares(const DistillParams& p, int row, Sh
     __syncthreads();
   }
   double mine = 0.0;
-  for (int e = tid; e < n; e += kSliceThreads) {
+  for (int e = tid; e < n; e += kShareThreads) {
     const int id = ids[e], g = e / p.k;
     const float v = values[e];
     double t = 0.0;
@@ -97,26 +107,7 @@ __device__ __forceinline__ double row_shares(const DistillParams& p, int row, Sh
     sh.t[e] = t;
     mine += t;
   }
-  return block_sum(mine, sh.warp);
-}
-
-// f(token, its whole share) for the listed tokens of the slice with a share, by whichever thread has the first entry.
-template <int DT, class F>
-__device__ __forceinline__ void each_listed(const DistillParams& p, const RowSlice<DT>& s, const Shares& sh, F&& f) {
-  const int n = p.lists * p.k;
-  const int lo = max(0, s.token(0)), hi = min(p.V, s.token(s.nv));
-  for (int e = threadIdx.x; e < n; e += kSliceThreads) {
-    const int id = sh.id[e];
-    if (id < lo || id >= hi) continue;
-    double t = 0.0;
-    bool first = true;
-    for (int j = 0; j < n; ++j)
-      if (sh.id[j] == id) {
-        first = first && j >= e;
-        t += sh.t[j];
-      }
-    if (first && t != 0.0) f(id, t);
-  }
+  return block_sum(mine, sh.per_warp);
 }
 
 template <int DT>
@@ -153,143 +144,219 @@ __device__ __forceinline__ uint4 packed(const float (&v)[Elem<DT>::E]) {
   return r;
 }
 
+// A vector of the gradient.
+template <int DT>
+__device__ __forceinline__ void write_vector(const RowSlice<DT>& s, char* row, int i, const float (&v)[Elem<DT>::E]) {
+  constexpr int E = Elem<DT>::E, B = Elem<DT>::bytes;
+  const int x = s.token(i);
+  if (static_cast<int>(reinterpret_cast<unsigned long long>(row) & 15) / B == s.off && x >= 0 && x <= s.V - E) {
+    *reinterpret_cast<uint4*>(row + static_cast<long long>(x) * B) = packed<DT>(v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (x + e >= 0 && x + e < s.V) store_entry<DT>(row, x + e, v[e]);
+  }
+}
 // The slice of the gradient: f(values) in place of the values.
 template <int DT, class F>
 __device__ __forceinline__ void write_slice(const RowSlice<DT>& s, char* row, bool read, F&& f) {
-  constexpr int E = Elem<DT>::E, B = Elem<DT>::bytes;
-  const bool whole = static_cast<int>(reinterpret_cast<unsigned long long>(row) & 15) / B == s.off;
+  constexpr int E = Elem<DT>::E;
   for (int i = s.begin + (threadIdx.x & 31); i < s.end; i += 32) {
     float v[E] = {};
     if (read) Elem<DT>::unpack(s.at(i), v);
     f(v);
-    const int x = s.token(i);
-    if (whole && x >= 0 && x <= s.V - E) {
-      *reinterpret_cast<uint4*>(row + static_cast<long long>(x) * B) = packed<DT>(v);
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (x + e >= 0 && x + e < s.V) store_entry<DT>(row, x + e, v[e]);
-    }
+    write_vector<DT>(s, row, i, v);
   }
 }
 
-// A part of a softmax normaliser: a sum of powers of two relative to the largest logit seen.
-struct Part {
+// The student's normaliser over the row: sum of 2^((s - m) c).
+struct Normaliser {
   float m;
-  double sum;
-  // a vector (NaN makes both NaN, +inf the sum)
-  template <int E>
-  __device__ __forceinline__ void add(const float (&v)[E], float c) {
-    float top = v[0];
-#pragma unroll
-    for (int e = 1; e < E; ++e) top = max_nan(top, v[e]);
-    if (top > m || top != top) {  // (a maximum that is NaN stays it)
-      sum *= static_cast<double>(m == -INFINITY ? 0.0f : ex2_approx((m - top) * c));
-      m = top;
-    }
-    if (m == -INFINITY) return;
-    float part = 0.0f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) part += ex2_approx((v[e] - m) * c);
-    sum += static_cast<double>(part);
-  }
+  double z;
 };
-
-struct Keep {
-  __device__ __forceinline__ u64 operator()(u64 a, u64) const { return a; }
+struct NormaliserRoom {
+  Normaliser warp[kSliceWarps], block[kSliceParts];
 };
-
-constexpr int kLoss = 0, kGrad = 1, kStep = 2;
-
-template <int DT, int MODE>
-__global__ void __launch_bounds__(kSliceThreads, 2) cos_distill_kernel(const DistillParams p) {
-  extern __shared__ uint4 smem[];
-  __shared__ Shares sh;
-  __shared__ Exchange x;
-  constexpr bool kCluster = MODE != kGrad;
+template <int DT>
+__device__ __forceinline__ Normaliser normaliser(NormaliserRoom& room, const RowSlice<DT>& s, int parts, int rank, float c) {
   constexpr int E = Elem<DT>::E;
-  const int parts = p.parts, rank = blockIdx.x % parts, row = blockIdx.x / parts, tid = threadIdx.x;
-  const bool wide = kCluster && parts > 1;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  float m = -INFINITY;
+  s.vectors([&](int, const float (&v)[E]) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) m = max_nan(m, v[e]);
+  });
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, d));
+  double z = 0.0;
+  if (!(m == -INFINITY))  // (NaN: all NaN)
+    s.vectors([&](int, const float (&v)[E]) {
+      float part = 0.0f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) part += ex2_approx((v[e] - m) * c);
+      z += static_cast<double>(part);
+    });
+  z = warp_sum(z);
+  if (lane == 0) room.warp[warp] = {m, z};
+  __syncthreads();
+  if (warp == 0) {
+    const Normaliser a = room.warp[lane & (kSliceWarps - 1)];
+    m = a.m;
+#pragma unroll
+    for (int d = kSliceWarps / 2; d > 0; d >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, d));
+    z = lane < kSliceWarps && a.m != -INFINITY ? a.z * static_cast<double>(ex2_approx((a.m - m) * c)) : 0.0;
+    z = warp_sum(z);
+    if (parts == 1) {
+      if (lane == 0) room.block[0] = {m, z};
+    } else if (lane < parts) {
+      *of_rank(&room.block[rank], lane) = {m, z};
+    }
+  }
+  row_barrier(parts);
+  Normaliser n = room.block[0];
+  for (int r = 1; r < parts; ++r) n.m = max_nan(n.m, room.block[r].m);
+  n.z = 0.0;
+  for (int r = 0; r < parts; ++r) {
+    const Normaliser a = room.block[r];
+    if (a.m != -INFINITY) n.z += a.z * static_cast<double>(ex2_approx((a.m - n.m) * c));
+  }
+  return n;
+}
+
+// q(x) times the scale, from the statistics of the student.
+template <int E>
+__device__ __forceinline__ void to_gradient(float (&v)[E], float scale, float m, float c, float log_z) {
+#pragma unroll
+  for (int e = 0; e < E; ++e) v[e] = scale * ex2_approx((v[e] - m) * c - log_z);
+}
+// The gradient at a listed token.
+__device__ __forceinline__ float listed_gradient(float s, double t, double per, double mass, float m, float c, float log_z) {
+  return static_cast<float>(per * (mass * exp2(static_cast<double>(s - m) * static_cast<double>(c) - static_cast<double>(log_z)) - t));
+}
+
+__device__ __forceinline__ Statistics* statistics_of(const DistillParams& p, int row) { return reinterpret_cast<Statistics*>(p.statistics) + row; }
+__device__ __forceinline__ float* shares_of(const DistillParams& p, int row) {  // (behind the statistics of all rows)
+  return p.statistics + static_cast<long long>(p.rows) * COS_DISTILL_STATISTICS + static_cast<long long>(row) * p.lists * p.k;
+}
+
+// The shares of a row: of a token's first entry its whole share, of the others 0.
+template <int DT>
+__global__ void __launch_bounds__(kShareThreads) cos_distill_shares_kernel(const DistillParams p) {
+  extern __shared__ uint4 smem[];
+  __shared__ double per_warp[kShareThreads / 32], list_max[COS_MAX_MODELS], list_sum[COS_MAX_MODELS];
+  wait_for_inputs();
+  asm volatile("griddepcontrol.launch_dependents;");  // (the rows: they read the student, which is settled where every block has come here)
+  const int row = blockIdx.x, n = p.lists * p.k;
+  const Shares sh = {reinterpret_cast<double*>(smem), reinterpret_cast<int*>(smem) + 2 * n, per_warp, list_max, list_sum};
+  const double mass = row_shares(p, row, sh);
+  if (!(mass != 0.0)) {  // nothing to learn from
+    if (threadIdx.x == 0) *statistics_of(p, row) = {0.0f, 0.0f, 0.0f, 0.0f, 0.0, 0.0};
+    return;
+  }
+  const char* student = p.student + static_cast<long long>(row) * p.stride * Elem<DT>::bytes;
+  int at = 0;
+  while (at < n && !(sh.t[at] != 0.0 && sh.id[at] < p.V)) ++at;
+  const float ref = at < n ? student_at<DT>(student, sh.id[at]) : 0.0f;
+  const double base = fabsf(ref) < INFINITY ? static_cast<double>(ref) : 0.0, inv_T = 1.0 / static_cast<double>(p.T);
+  float* const shares = shares_of(p, row);
+  double listed = 0.0;
+  for (int e = threadIdx.x; e < n; e += kShareThreads) {
+    const int id = sh.id[e];
+    double t = 0.0;
+    if (id >= 0 && id < p.V) {
+      bool first = true;
+#pragma unroll 4
+      for (int j = 0; j < n; ++j)
+        if (sh.id[j] == id) {
+          first = first && j >= e;
+          t += sh.t[j];
+        }
+      if (!first) t = 0.0;
+      if (t != 0.0) listed += t * (log(t) - (static_cast<double>(student_at<DT>(student, id)) - base) * inv_T);
+    }
+    shares[e] = static_cast<float>(t);
+  }
+  listed = block_sum(listed, per_warp);
+  if (threadIdx.x == 0) *statistics_of(p, row) = {0.0f, 0.0f, static_cast<float>(mass), static_cast<float>(base), listed, mass};
+}
+
+// The rows.  kGrad: the normalisers are there, and every block works for itself.
+template <int DT, int MODE>
+__global__ void __launch_bounds__(kSliceThreads, 3) cos_distill_kernel(const DistillParams p) {
+  extern __shared__ uint4 smem[];
+  __shared__ NormaliserRoom room;
+  constexpr int E = Elem<DT>::E;
+  const int parts = p.parts, rank = blockIdx.x % parts, row = blockIdx.x / parts, tid = threadIdx.x, n = p.lists * p.k;
+  const bool wide = MODE != kGrad && parts > 1;
   if (wide) cluster_barrier_arrive();
-  int turn = 0;
   const char* student = p.student + static_cast<long long>(row) * p.stride * Elem<DT>::bytes;
   char* grad = MODE != kLoss ? p.grad + static_cast<long long>(row) * p.stride_grad * Elem<DT>::bytes : nullptr;
   RowSlice<DT> s;
   s.init(student, p.V, rank, p.share, p.seg, smem, p.res);
+  const bool early = MODE != kGrad && blockIdx.x < p.early;
+  if (early) s.start();
+  wait_for_inputs();
+  const Statistics st = *statistics_of(p, row);
   const float weight = MODE != kLoss ? p.row_weights[row] : 1.0f;
-  const double mass = row_shares(p, row, sh);  // (the same in every block)
-  const float nan = __int_as_float(0x7fc00000);
-
-  if (!(mass != 0.0) || (MODE == kGrad && weight == 0.0f)) {  // nothing to learn from
-    if (MODE != kGrad && rank == 0 && tid == 0) {
-      p.loss[row] = 0.0f;
-      if (MODE == kLoss) p.statistics[row] = make_float2(0.0f, 0.0f);
-    }
+  const bool none = st.mass64 == 0.0;
+  if (none || (MODE == kGrad && weight == 0.0f)) {
+    if (MODE != kGrad && rank == 0 && tid == 0) p.loss[row] = 0.0f;
     if (MODE != kLoss) write_slice<DT>(s, grad, false, [](float (&)[E]) {});
+    s.finish();
     if (wide) cluster_barrier_wait();
     return;
   }
-
+  if (!early) s.start();
+  // the listed tokens of the slice, before the gradient takes their place
+  struct Listed {
+    int id;
+    float s, t;
+  } mine[2] = {{-1, 0.0f, 0.0f}, {-1, 0.0f, 0.0f}};
+  static_assert(2 * kSliceThreads >= COS_TOP_MAX, "a thread has two entries at most");
+  if (MODE != kLoss) {
+    const int lo = max(0, s.token(0)), hi = min(p.V, s.token(s.nv));
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int e = tid + k * kSliceThreads;
+      if (e < n) {
+        const int id = p.ids[static_cast<long long>(row) * n + e];
+        const float t = shares_of(p, row)[e];
+        if (id >= lo && id < hi && t != 0.0f) mine[k] = {id, student_at<DT>(student, id), t};
+      }
+    }
+  }
+  s.finish();
   const float c = fminf(static_cast<float>(1.4426950408889634 / static_cast<double>(p.T)), 3e38f);
-  float m, log_z;
-  if constexpr (MODE != kGrad) {
-    Part part = {-INFINITY, 0.0};
-    s.load([&](const float (&v)[E]) { part.add(v, c); });
-    if (wide) cluster_barrier_wait();
-    const auto larger = [](u64 a, u64 b) {
-      return static_cast<u64>(__float_as_uint(max_nan(__uint_as_float(static_cast<unsigned>(a)), __uint_as_float(static_cast<unsigned>(b)))));
-    };
-    const auto add = [](u64 a, u64 b) {
-      return static_cast<u64>(__double_as_longlong(__longlong_as_double(static_cast<long long>(a)) + __longlong_as_double(static_cast<long long>(b))));
-    };
-    m = __uint_as_float(static_cast<unsigned>(exchange(x, turn, parts, rank, __float_as_uint(part.m), 0, larger, Keep()).a));
-    // of the listed tokens, relative to the largest logit: t (ln t - (s - m) / T)
-    double listed = 0.0;
-    each_listed(p, s, sh, [&](int id, double t) { listed += t * (log(t) - (static_cast<double>(student_at<DT>(student, id)) - static_cast<double>(m)) / static_cast<double>(p.T)); });
-    const double mine = part.m == -INFINITY ? 0.0 : part.sum * static_cast<double>(ex2_approx((part.m - m) * c));
-    const Words sums = exchange(x, turn, parts, rank, static_cast<u64>(__double_as_longlong(mine)), static_cast<u64>(__double_as_longlong(listed)), add, add);
-    const double z = __longlong_as_double(static_cast<long long>(sums.a));
-    log_z = m == -INFINITY ? nan : static_cast<float>(log2(z));
+  float m = st.m, log_z = st.log_z;
+  if (MODE != kGrad) {
+    if (wide) cluster_barrier_wait();  // (every block of the row has started)
+    const Normaliser z = normaliser<DT>(room, s, parts, rank, c);
+    const bool empty = z.m == -INFINITY;
+    m = z.m;
+    log_z = empty ? __int_as_float(0x7fc00000) : static_cast<float>(log2(z.z));
     if (rank == 0 && tid == 0) {
-      p.loss[row] = m == -INFINITY ? nan : static_cast<float>(__longlong_as_double(static_cast<long long>(sums.b)) + mass * log(z));
-      if (MODE == kLoss) p.statistics[row] = make_float2(m, log_z);
+      const double inv_T = 1.0 / static_cast<double>(p.T);
+      p.loss[row] = empty ? log_z : static_cast<float>(st.listed + st.mass64 * ((static_cast<double>(m) - static_cast<double>(st.reference)) * inv_T + log(z.z)));
+      if (MODE == kLoss) {
+        statistics_of(p, row)->m = m;
+        statistics_of(p, row)->log_z = log_z;
+      }
     }
   } else {
-    const float2 st = p.statistics[row];
-    m = st.x;
-    log_z = st.y;
+    __syncthreads();  // (the listed tokens have been read)
   }
-  if constexpr (MODE != kLoss) {
+  if (MODE != kLoss) {
     if (MODE == kStep && weight == 0.0f) {
       write_slice<DT>(s, grad, false, [](float (&)[E]) {});
       return;
     }
-    const double per = static_cast<double>(weight) / static_cast<double>(p.T);
+    const double per = static_cast<double>(weight) / static_cast<double>(p.T), mass = static_cast<double>(st.mass);
     const float scale = static_cast<float>(per * mass);
-    // the listed tokens of the slice, before the gradient takes their place
-    struct Listed {
-      int id;
-      float g;
-    } at[2] = {{-1, 0.0f}, {-1, 0.0f}};
-    static_assert(2 * kSliceThreads >= COS_TOP_MAX, "a thread has two entries at most");
-    int found = 0;
-    each_listed(p, s, sh, [&](int id, double t) {
-      const double q = exp2(static_cast<double>(student_at<DT>(student, id) - m) * static_cast<double>(c) - static_cast<double>(log_z));
-      const Listed l = {id, static_cast<float>(per * (mass * q - t))};
-      if (found++ == 0)
-        at[0] = l;
-      else
-        at[1] = l;
-    });
-    __syncthreads();
-    write_slice<DT>(s, grad, true, [&](float (&v)[E]) {
+    write_slice<DT>(s, grad, true, [&](float (&v)[E]) { to_gradient(v, scale, m, c, log_z); });
+    __syncthreads();  // (the listed tokens' places are written again)
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[e] = scale * ex2_approx((v[e] - m) * c - log_z);
-    });
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      if (at[i].id >= 0) store_entry<DT>(grad, at[i].id, at[i].g);
+    for (int k = 0; k < 2; ++k)
+      if (mine[k].id >= 0) store_entry<DT>(grad, mine[k].id, listed_gradient(mine[k].s, static_cast<double>(mine[k].t), per, mass, m, c, log_z));
   }
 }
 
@@ -310,7 +377,7 @@ cos_status distill(const cos_distill_args* a, void* cuda_stream) {
   const int bytes = a->dtype == COS_DTYPE_F32 ? 4 : 2;
   if (misaligned(a->student, bytes)) return call_failed(COS_ERR_ALIGNMENT, "student pointer not aligned to its element type");
   if (MODE != kGrad && !a->loss) return call_failed(COS_ERR_INVALID_ARG, "null device pointer");
-  if (MODE != kStep && !a->statistics) return call_failed(COS_ERR_INVALID_ARG, "null device pointer");
+  if (!a->statistics) return call_failed(COS_ERR_INVALID_ARG, "null device pointer");
   if (MODE != kLoss) {
     if (!a->row_weights || !a->grad) return call_failed(COS_ERR_INVALID_ARG, "null device pointer");
     if (misaligned(a->grad, bytes)) return call_failed(COS_ERR_ALIGNMENT, "grad pointer not aligned to its element type");
@@ -319,12 +386,12 @@ cos_status distill(const cos_distill_args* a, void* cuda_stream) {
   }
   if (misaligned(a->ids, 4) || misaligned(a->values, 4) || misaligned(a->lse, 4) || (MODE != kGrad && misaligned(a->loss, 4)) || (MODE != kLoss && misaligned(a->row_weights, 4)))
     return call_failed(COS_ERR_ALIGNMENT, "an int32/float pointer is not 4-byte aligned");
-  if (MODE != kStep && misaligned(a->statistics, 8)) return call_failed(COS_ERR_ALIGNMENT, "statistics is not 8-byte aligned");
+  if (misaligned(a->statistics, 16)) return call_failed(COS_ERR_ALIGNMENT, "statistics is not 16-byte aligned");
 
   OnDevice on(a->device);
   if (on.error != cudaSuccess) return call_failed("cudaSetDevice", on.error);
   SlicePlan plan;
-  cudaError_t e = slice_plan(a->device, a->rows, a->vocab, a->dtype, &plan);
+  cudaError_t e = slice_plan(a->device, a->rows, a->vocab, a->dtype, 64 * 1024, MODE != kGrad, &plan);
   if (e != cudaSuccess) return call_failed("device query", e);
   if (static_cast<long long>(a->rows) * plan.parts > 0x7fffffffll) return call_failed(COS_ERR_UNSUPPORTED, "too many rows for one launch");
   DistillParams p = {};
@@ -335,7 +402,8 @@ cos_status distill(const cos_distill_args* a, void* cuda_stream) {
   p.parts = plan.parts;
   p.share = plan.share;
   p.seg = plan.seg;
-  p.res = MODE == kStep ? plan.res : 0;
+  p.res = plan.res;
+  p.early = 2 * plan.sms;
   p.lists = a->lists;
   p.k = a->k;
   p.ids = a->ids;
@@ -345,13 +413,21 @@ cos_status distill(const cos_distill_args* a, void* cuda_stream) {
   p.T = a->temperature;
   p.row_weights = a->row_weights;
   p.loss = a->loss;
-  p.statistics = reinterpret_cast<float2*>(a->statistics);
+  p.statistics = a->statistics;
   p.grad = static_cast<char*>(a->grad);
   p.stride_grad = a->stride_grad;
-  void (*fn)(DistillParams) = a->dtype == COS_DTYPE_F32    ? cos_distill_kernel<COS_DTYPE_F32, MODE>
-                              : a->dtype == COS_DTYPE_BF16 ? cos_distill_kernel<COS_DTYPE_BF16, MODE>
-                                                           : cos_distill_kernel<COS_DTYPE_F16, MODE>;
-  e = slice_launch(fn, p, a->rows * plan.parts, MODE == kGrad ? 1 : plan.parts, MODE == kStep ? plan.smem : 0, static_cast<cudaStream_t>(cuda_stream));
+  const auto launches = [&](auto dt) {
+    constexpr int DT = decltype(dt)::value;
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (MODE != kGrad) {
+      const cudaError_t first = slice_launch(cos_distill_shares_kernel<DT>, p, a->rows, 1, static_cast<size_t>(a->lists) * a->k * (sizeof(double) + sizeof(int)), stream, kShareThreads);
+      if (first != cudaSuccess) return first;
+    }
+    return slice_launch(cos_distill_kernel<DT, MODE>, p, a->rows * plan.parts, MODE == kGrad ? 1 : plan.parts, plan.smem, stream);
+  };
+  e = a->dtype == COS_DTYPE_F32    ? launches(std::integral_constant<int, COS_DTYPE_F32>())
+      : a->dtype == COS_DTYPE_BF16 ? launches(std::integral_constant<int, COS_DTYPE_BF16>())
+                                   : launches(std::integral_constant<int, COS_DTYPE_F16>());
   return e == cudaSuccess ? COS_OK : call_failed("launch", e);
 }
 

@@ -2,20 +2,31 @@
 // cluster of blocks a row (cos_slice.cuh).
 //
 // Mathematics.  In order of (logit down, index up) every one of the three limits keeps a beginning of the line, so what is kept is the tokens at or
-// above one of them; a token's place in the line is one 64-bit number (`place_of`).  The limit is found by a histogram of 2048 bins, linear in the
-// logit below the maximum: the bin in which the k-th token lies, or the one in which the sum of the weights reaches p, then (usually a handful of tokens)
-// the places in that bin against each other.  A bin of more than kCandidates is cut into 2048 ranges of places, again until few are left: places
-// are 64 bits and no two are alike, so this ends after at most six histograms, for any number of equal logits.
+// above one of them.  A token's place in the line is one 64-bit number (`place_of`).
 //
-// Weights are exp2 of 64-bit arguments, from a table of 2^(j/64) and the power series of 2^r for |r| <= 1/128 (the fifth term is below 4e-14), rounded to
-// whole multiples of 2^-scale and summed as integers: a token is drawn where a border of the cumulative sums lies next to u, and 32-bit sums are off by more
-// than the weight of a token there.  Integers make sums independent of their order, so atomics and the split over blocks change nothing.
+// The head of the line is found without sorting or counting tokens: of 512 groups of tokens (the same for all blocks) each block gets the largest logit; the
+// k-th largest of these is at most the k-th largest logit, and little below it (k of 512 groups are taken up by some -512 ln(1 - k/512) tokens: 53 for k = 50).
+// The few tokens from there on are compared with one another, and where the limits lie among them the row is done (top-k up to kHeadMost; top-p whose tokens
+// are among the first few hundred).  Else a histogram of 1024 bins, linear in the logit below the maximum, says in which bin a limit lies, and the places in
+// that bin are compared; a bin of more than kCandidates is cut into 1024 ranges of places, again until few are left: places are 64 bits and no two are alike,
+// so this ends after at most seven histograms, for any number of equal logits.
+//
+// Weights are exp2 of 64-bit arguments (2^-36 of the largest and less: of 32-bit ones, off by 2^-17 of themselves), from a table of 2^(j/512) and the power
+// series of 2^r for |r| <= 2^-10 (the fourth term is below 1e-14), rounded to whole multiples of 2^-scale and summed as integers: a token is drawn where a
+// border of the cumulative sums lies next to u, and 32-bit sums are off by more than the weight of a token there.  Integers make sums independent of their
+// order, so atomics and the split over blocks change nothing.
 #include "cos_slice.cuh"
 
 namespace cosv {
 namespace {
 
-constexpr int kBins = 2048, kCandidates = 512, kTopCandidates = COS_TOP_MAX + 512;
+constexpr int kBins = 1024, kBinBits = 10, kCandidates = 512, kTopCandidates = COS_TOP_MAX + 512;
+// the largest k that a list of that size is used for
+template <int kList>
+constexpr int kMost = kList == kTopCandidates ? COS_TOP_MAX : 288;
+constexpr int kFew = 128;
+constexpr int kHeadMost = kMost<kCandidates>, kHeadGuess = 96;  // the largest top-k that the head is tried for; the k it is tried with for a top-p alone
+static_assert(kCandidates == kSliceThreads, "a thread for each");
 
 struct Common {  // of both kernels
   const void* logits;
@@ -58,26 +69,91 @@ __device__ __forceinline__ u64 place_of(float v, int token) { return static_cast
 __device__ __forceinline__ float logit_at(u64 place) { return unordered(static_cast<unsigned>(place >> 32)); }
 __device__ __forceinline__ int token_at(u64 place) { return static_cast<int>(0xffffffffu - static_cast<unsigned>(place)); }
 
-// exp((l - m) / T) in units of 2^-scale.
+constexpr int kTable = 512;
+constexpr float kNear = 36.0f;
+
+// exp((l - m) / T) in whole multiples of 2^-scale.
+template <int DT>
 struct Weight {
-  double m, c;       // the row's largest logit, log2(e) / T
-  const double* table;  // 2^(j / 64)
+  float half, c32x2;    // half the row's largest logit (differences of halves do not overflow), twice log2(e) / T
+  double m64, c;        // the logit, log2(e) / T
+  const double* table;  // 2^(j / 512)
   int scale;
-  __device__ __forceinline__ double of(float l) const {  // not rounded to the unit; l is finite
-    constexpr double kRound = 105553116266496.0;         // 1.5 * 2^46: sums with it are multiples of 2^-6
-    const double t = fmax((static_cast<double>(l) - m) * c, -900.0);
-    const double k = t + kRound;
-    const double r = t - (k - kRound);
+  // A finite float widened (0 and subnormal numbers to next to nothing): integer instructions, of which there are eight times as many a clock as conversions.
+  static __device__ __forceinline__ double widen(float v) {
+    const unsigned u = __float_as_uint(v);
+    return __hiloint2double(static_cast<int>((((u & 0x7fffffffu) >> 3) + 0x38000000u) | (u & 0x80000000u)), DT == COS_DTYPE_F32 ? static_cast<int>(u << 29) : 0);
+  }
+  __device__ __forceinline__ void init(float m, float T, int V, const double* table_) {
+    half = 0.5f * m;
+    m64 = widen(m);
+    c = 1.4426950408889634 / static_cast<double>(T);
+    c32x2 = fmaxf(fminf(static_cast<float>(2.0 * c), 3e38f), 1e-37f);  // (-inf is infinitely far at any temperature)
+    table = table_;
+    scale = min(46, 63 - (32 - __clz(V - 1)));
+  }
+  // Powers of two that l's weight is below the largest.
+  __device__ __forceinline__ float below(float l) const { return fmaf(-0.5f, l, half) * c32x2; }
+  // 2^(i / 512) units
+  __device__ __forceinline__ double power(int i) const {
+    const double e = table[i & (kTable - 1)];
+    return __hiloint2double(__double2hiint(e) + (((i >> 9) + scale) << 20), __double2loint(e));
+  }
+  // Not rounded to the unit; l is at most 2^40 units of the temperature below the largest.
+  __device__ __forceinline__ double exact(float l) const {
+    constexpr double kRound = 13194139533312.0;  // 1.5 * 2^43: sums with it are multiples of 2^-9
+    const double d = widen(l) - m64;
+    const double k = fma(d, c, kRound);
+    const double r = fma(d, c, kRound - k);
     const int n = __double2loint(k);
-    double e = fma(0.009618129107628477, r, 0.05550410866482158);  // ln(2)^i / i!
-    e = fma(e, r, 0.2402265069591007);
+    double e = fma(0.05550410866482158, r, 0.2402265069591007);  // ln(2)^i / i!
     e = fma(e, r, 0.6931471805599453);
     e = fma(e, r, 1.0);
-    e *= table[n & 63];
-    return __hiloint2double(__double2hiint(e) + (((n >> 6) + scale) << 20), __double2loint(e));
+    e *= table[n & (kTable - 1)];
+    return __hiloint2double(__double2hiint(e) + (((n >> 9) + scale) << 20), __double2loint(e));
   }
-  static __device__ __forceinline__ u64 whole(double w) {  // w <= 2^46
-    return static_cast<u64>(__double_as_longlong(w + 4503599627370496.0)) & 0xfffffffffffffull;
+  __device__ __forceinline__ u64 near(float l) const {  // below(l) < kNear; at most 2^46
+    return static_cast<u64>(__double_as_longlong(exact(l) + 4503599627370496.0)) & 0xfffffffffffffull;
+  }
+  __device__ __forceinline__ unsigned far(float x) const {  // x = below(l) >= kNear; at most 2^10
+    return __float_as_uint(ex2_approx(static_cast<float>(scale) - x) + 8388608.0f) - 0x4b000000u;
+  }
+  // l is not +inf or NaN; 0 for -inf.
+  __device__ __forceinline__ u64 of(float l) const {
+    const float x = below(l);
+    return x < kNear ? near(l) : far(x);
+  }
+  // Sum over the entries of a vector that keep(value, token) holds of.  Those far below the largest go by 32 bits, all at once; the others one by one (two under
+  // way), by 64-bit instructions that take half the time of a sweep where most entries are near, and next to none where few are.
+  template <class K>
+  __device__ __forceinline__ u64 of_vector(const uint4& r, int token, K&& keep) const {
+    constexpr int E = Elem<DT>::E;
+    unsigned tail = 0, head = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const float v = entry<DT>(r, e), x = below(v);
+      const bool kept = keep(v, token + e);
+      if (kept && x < kNear) head |= 1u << e;
+      tail += kept && x >= kNear ? far(x) : 0u;
+    }
+    u64 sum = tail;
+    while (head) {
+      const int a = __ffs(head) - 1;
+      head &= head - 1;
+      const int b = head ? __ffs(head) - 1 : -1;
+      head &= head - 1;
+      const u64 wa = near(pick(r, a)), wb = near(pick(r, b < 0 ? a : b));
+      sum += wa + (b < 0 ? 0ull : wb);
+    }
+    return sum;
+  }
+  static __device__ __forceinline__ float pick(const uint4& r, int e) {
+    const int i = DT == COS_DTYPE_F32 ? e : e >> 1;
+    const unsigned lo = (i & 1) ? r.y : r.x, hi = (i & 1) ? r.w : r.z, w = (i & 2) ? hi : lo;
+    if (DT == COS_DTYPE_F32) return __uint_as_float(w);
+    const unsigned h = (e & 1) ? w >> 16 : w & 0xffffu;
+    if (DT == COS_DTYPE_BF16) return __uint_as_float(h << 16);
+    return __half2float(__ushort_as_half(static_cast<unsigned short>(h)));
   }
 };
 
@@ -86,89 +162,81 @@ struct Found {
   int bin, there;
 };
 
-template <int kList, int kMasses>
-struct Histogram {
-  unsigned count[kBins], mass_lo[kBins], mass_hi[kBins];
-  u64 list[kList];    // this block's candidates
-  u64 merged[kList];  // the row's
-  u64 mass[kMasses];
+template <int kList>
+struct Shared {
+  unsigned count[kBins], lo[kBins], hi[kBins];
+  u64 list[kList];             // this block's candidates
+  u64 merged[kList];           // the row's
+  u64 order[kFew];             // ... sorted, where they are few
+  float group[kSliceThreads];  // the largest logit of each group of the row
   u64 scan_count[kSliceWarps], scan_mass[kSliceWarps];
-  int listed, pad[3];
   Found found[2];
+  u64 word[2];
+  unsigned steps[64];
+  int listed, pad[3];
 };
+using SampleShared = Shared<kCandidates>;
+static_assert(sizeof(SampleShared) % 16 == 0 && sizeof(Shared<kTopCandidates>) % 16 == 0, "the slice lies behind it");
 
-using SampleShared = Histogram<kCandidates, kCandidates>;
-using TopShared = Histogram<kTopCandidates, 2>;
-static_assert(sizeof(SampleShared) % 16 == 0 && sizeof(TopShared) % 16 == 0, "the slice lies behind it");
-
-// The bins of this block's share of the row's histogram, four a thread at most, with what lies before them in the line.
+constexpr int kBinsEach = kBins / kSliceThreads;
+// The bins of this block's share of the row's histogram, with what lies before them in the line.
 struct Bins {
   int first, n;  // this thread's
-  u64 count[4], mass[4], before_count, before_mass;
+  u64 count[kBinsEach], mass[kBinsEach], before_count, before_mass;
   u64 all_count, all_mass;  // of the row
 };
 
+// What is the same for every step of a row.
 template <class H>
-__device__ __forceinline__ void clear_bins(H& h, bool masses) {
-  for (int i = threadIdx.x; i < kBins; i += kSliceThreads) {
-    h.count[i] = 0;
-    if (masses) h.mass_lo[i] = h.mass_hi[i] = 0;
-  }
-  __syncthreads();
+struct Row {
+  H& h;
+  Exchange& x;
+  int parts, rank, turn, slot;
+};
+
+template <class H>
+__device__ __forceinline__ void clear_bins(H& h) {
+  for (int i = threadIdx.x; i < kBins; i += kSliceThreads) h.count[i] = h.lo[i] = h.hi[i] = 0;
 }
 
-template <class H>
-__device__ __forceinline__ void add_to_bin(H& h, int bin, bool masses, u64 w) {
-  atomicAdd(&h.count[bin], 1u);
-  if (masses) {  // 64 bits in two words: whoever makes the low one overflow carries
-    const unsigned lo = static_cast<unsigned>(w);
-    const unsigned was = atomicAdd(&h.mass_lo[bin], lo);
-    const unsigned hi = static_cast<unsigned>(w >> 32) + (was + lo < was ? 1u : 0u);
-    if (hi) atomicAdd(&h.mass_hi[bin], hi);
-  }
-}
-
-struct Add {
-  __device__ __forceinline__ u64 operator()(u64 a, u64 b) const { return a + b; }
-};
-struct Max {
-  __device__ __forceinline__ u64 operator()(u64 a, u64 b) const { return a > b ? a : b; }
-};
-struct Min {
-  __device__ __forceinline__ u64 operator()(u64 a, u64 b) const { return a < b ? a : b; }
-};
-
-// Behind the sweep that filled the blocks' bins: the sums over the blocks, in order.  The bins may be cleared afterwards.
-template <class H>
-__device__ __forceinline__ void merge_bins(H& h, Exchange& x, int& turn, int parts, int rank, bool masses, Bins& b) {
-  row_barrier(parts);
-  const int own = kBins / parts, each = own > kSliceThreads ? own / kSliceThreads : 1;
+// Behind the sweep that filled the blocks' bins and a barrier of the row: the sums over the blocks, in order, with mass_of(bin, count, lo, hi) for a bin.  The
+// bins may be cleared afterwards.
+template <class H, class M>
+__device__ __forceinline__ void merge_bins(Row<H>& w, bool masses, bool wide, Bins& b, M&& mass_of) {
+  const int own = kBins / w.parts, each = own > kSliceThreads ? own / kSliceThreads : 1;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   b.n = tid * each < own ? each : 0;
-  b.first = rank * own + tid * each;
+  b.first = w.rank * own + tid * each;
   u64 count = 0, mass = 0;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
+  for (int q = 0; q < kBinsEach; ++q) {
     b.count[q] = b.mass[q] = 0;
     if (q < b.n) {
-      if (parts == 1) {
-        b.count[q] = h.count[b.first + q];
-        if (masses) b.mass[q] = static_cast<u64>(h.mass_hi[b.first + q]) << 32;
-        if (masses) b.mass[q] += h.mass_lo[b.first + q];
+      const int i = b.first + q;
+      unsigned n = 0;
+      u64 lo = 0;
+      unsigned hi = 0;
+      if (w.parts == 1) {
+        n = w.h.count[i];
+        lo = w.h.lo[i];
+        hi = w.h.hi[i];
       } else {
-#pragma unroll 4
-        for (int r = 0; r < parts; ++r) {
-          const H* o = of_rank(&h, r);
-          b.count[q] += o->count[b.first + q];
-          if (masses) b.mass[q] += (static_cast<u64>(o->mass_hi[b.first + q]) << 32) + o->mass_lo[b.first + q];
-        }
+#pragma unroll
+        for (int r = 0; r < kSliceParts; ++r)  // (all under way at once)
+          if (r < w.parts) {
+            const H* o = of_rank(&w.h, r);
+            n += o->count[i];
+            if (masses) lo += o->lo[i];
+            if (wide) hi += o->hi[i];
+          }
       }
+      b.count[q] = n;
+      if (masses) b.mass[q] = mass_of(i, n, lo, hi);
     }
     count += b.count[q];
     mass += b.mass[q];
   }
-  // exclusive scan over the block
-  u64 sc = count, sm = mass;
+  u64 sc = count, sm = mass;  // exclusive scan over the block
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
     const u64 c = __shfl_up_sync(0xffffffffu, sc, d), m = __shfl_up_sync(0xffffffffu, sm, d);
@@ -178,73 +246,93 @@ __device__ __forceinline__ void merge_bins(H& h, Exchange& x, int& turn, int par
     }
   }
   if (lane == 31) {
-    h.scan_count[warp] = sc;
-    h.scan_mass[warp] = sm;
+    w.h.scan_count[warp] = sc;
+    w.h.scan_mass[warp] = sm;
   }
-  const int t = turn & 1;
-  exchange(x, turn, parts, rank, count, mass, Add(), Add());  // (its barriers are this scan's too)
+  const int t = w.turn & 1;
+  exchange<Add, Add>(w.x, w.turn, w.parts, w.rank, count, mass);  // (its barriers are this scan's too)
   sc -= count;
   sm -= mass;
-  for (int w = 0; w < warp; ++w) {
-    sc += h.scan_count[w];
-    sm += h.scan_mass[w];
-  }
-  b.all_count = b.all_mass = 0;
-  for (int r = 0; r < parts; ++r) {
-    if (r < rank) {
-      sc += x.a[t][r];
-      sm += x.b[t][r];
-    }
-    b.all_count += x.a[t][r];
-    b.all_mass += x.b[t][r];
-  }
-  b.before_count = sc;
-  b.before_mass = sm;
+  // (what the warps and blocks before this one have, and the row: by every warp at once)
+  sc += Add::warp(lane < warp ? w.h.scan_count[lane & (kSliceWarps - 1)] : 0);
+  sm += Add::warp(lane < warp ? w.h.scan_mass[lane & (kSliceWarps - 1)] : 0);
+  const u64 ac = lane < w.parts ? w.x.a[t][lane & (kSliceParts - 1)] : 0, am = lane < w.parts ? w.x.b[t][lane & (kSliceParts - 1)] : 0;
+  b.before_count = sc + Add::warp(lane < w.rank ? ac : 0);
+  b.before_mass = sm + Add::warp(lane < w.rank ? am : 0);
+  b.all_count = Add::warp(ac);
+  b.all_mass = Add::warp(am);
 }
 
-// The bin in which the `target`-th token (by_mass: unit of mass) lies; 1 <= target <= what the row has.  `slot`: used in turns.
+// The bin in which the `target`-th token (by_mass: unit of mass) lies; 1 <= target <= what the row has.
 template <class H>
-__device__ __forceinline__ Found locate(H& h, const Bins& b, int parts, bool by_mass, u64 target, int slot) {
+__device__ __forceinline__ Found locate(Row<H>& w, const Bins& b, bool by_mass, u64 target) {
+  const int slot = w.slot;
+  w.slot ^= 1;
   u64 c = b.before_count, m = b.before_mass;
+  Found f = {0, 0, 0, 0, 0};
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
+  for (int q = 0; q < kBinsEach; ++q) {
     const u64 at = by_mass ? m : c, here = by_mass ? b.mass[q] : b.count[q];
-    if (q < b.n && at < target && target <= at + here) {
-      const Found f = {c, m, b.count[q], b.first + q, 1};
-      if (parts == 1)
-        h.found[slot] = f;
-      else
-        for (int r = 0; r < parts; ++r) *of_rank(&h.found[slot], r) = f;
-    }
+    if (q < b.n && at < target && target <= at + here) f = {c, m, b.count[q], b.first + q, 1};
     c += b.count[q];
     m += b.mass[q];
   }
-  row_barrier(parts);
-  return h.found[slot];
+  const unsigned who = __ballot_sync(0xffffffffu, f.there);
+  if (who) {  // (one lane of the row: its warp tells every block)
+    const int src = __ffs(who) - 1, lane = threadIdx.x & 31;
+    f.before_count = __shfl_sync(0xffffffffu, f.before_count, src);
+    f.before_mass = __shfl_sync(0xffffffffu, f.before_mass, src);
+    f.count = __shfl_sync(0xffffffffu, f.count, src);
+    f.bin = __shfl_sync(0xffffffffu, f.bin, src);
+    if (w.parts == 1) {
+      if (lane == 0) w.h.found[slot] = f;
+    } else if (lane < w.parts) {
+      *of_rank(&w.h.found[slot], lane) = f;
+    }
+  }
+  row_barrier(w.parts);
+  return w.h.found[slot];
 }
 
-// The places of the tokens that `in` holds, all of them to every block of the row: h.merged[0 .. n).  There are no more than the list has room for.
-template <class H, class S, class In>
-__device__ __forceinline__ int gather(H& h, Exchange& x, int& turn, int parts, int rank, const S& s, In&& in) {
-  if (threadIdx.x == 0) h.listed = 0;
+// Lists a candidate of this block (as many as there is room for).
+template <class H>
+__device__ __forceinline__ void list(H& h, float v, int token) {
+  const int at = atomicAdd(&h.listed, 1);
+  if (at < static_cast<int>(sizeof(h.list) / sizeof(u64))) h.list[at] = place_of(v, token);
+}
+// Behind the sweep that listed them (h.listed was 0): how many candidates the row has, and the sums over the row of `sum` and of the lanes' masses of what
+// they listed.
+struct Taken {
+  u64 n, sum, listed;
+};
+template <class Sum = Nothing, class Listed = Nothing, class H>
+__device__ __forceinline__ Taken taken(Row<H>& w, u64 sum = 0, u64 listed = 0) {
   __syncthreads();
-  s.sweep([&](int token, const auto& v) {
-#pragma unroll
-    for (int e = 0; e < S::E; ++e)
-      if (in(v[e], token + e)) h.list[atomicAdd(&h.listed, 1)] = place_of(v[e], token + e);
-  });
-  __syncthreads();
-  const int mine = h.listed, t = turn & 1;
-  exchange(x, turn, parts, rank, threadIdx.x == 0 ? mine : 0, 0, Add(), Add());
-  int n = 0;
-  for (int r = 0; r < parts; ++r) n += static_cast<int>(x.a[t][r]);
+  const Words all = exchange<OfFirst, Sum, Listed>(w.x, w.turn, w.parts, w.rank, static_cast<u64>(w.h.listed), sum, listed);
+  if (threadIdx.x == 0) w.h.listed = 0;  // (for the next one: behind a barrier of the row, and ahead of one of the block)
+  return {all.a, all.b, all.c};
+}
+// ... and the candidates of all blocks, n of them, to this one: right behind take().
+template <class H>
+__device__ __forceinline__ void merge_lists(Row<H>& w, int n) {
+  const int t = (w.turn - 1) & 1;
   for (int i = threadIdx.x; i < n; i += kSliceThreads) {
-    int r = 0, j = i;
-    while (j >= static_cast<int>(x.a[t][r])) j -= static_cast<int>(x.a[t][r++]);
-    h.merged[i] = parts == 1 ? h.list[j] : *of_rank(&h.list[j], r);
+    if (w.parts == 1) {
+      w.h.merged[i] = w.h.list[i];
+      continue;
+    }
+    int r = 0, j = i, before = 0;
+#pragma unroll
+    for (int q = 0; q < kSliceParts - 1; ++q)
+      if (q < w.parts - 1) {
+        before += static_cast<int>(w.x.a[t][q]);
+        if (i >= before) {
+          r = q + 1;
+          j = i - before;
+        }
+      }
+    w.h.merged[i] = *of_rank(&w.h.list[j], r);
   }
-  __syncthreads();
-  return n;
 }
 
 // Where in the line a bin's tokens lie, cut down until no more than `most` of them are left.
@@ -252,36 +340,41 @@ struct Range {
   u64 lo, hi;  // places, inclusive
   u64 before_count, before_mass, count;
 };
-template <class H, class S, class In>
-__device__ __forceinline__ Range narrow(H& h, Exchange& x, int& turn, int& slot, int parts, int rank, const S& s, const Weight* w, bool by_mass, u64 target, const Found& f, u64 most, In&& in) {
-  Range g = {~0ull, 0, f.before_count, f.before_mass, f.count};
-  s.sweep([&](int token, const auto& v) {
-#pragma unroll
-    for (int e = 0; e < S::E; ++e)
-      if (in(v[e], token + e)) {
-        const u64 at = place_of(v[e], token + e);
-        g.lo = at < g.lo ? at : g.lo;
-        g.hi = at > g.hi ? at : g.hi;
-      }
+template <class H, class S, class W, class In>
+__device__ __forceinline__ Range narrow(Row<H>& w, const S& s, W&& weight, bool by_mass, u64 target, Range g, u64 most, In&& in) {
+  u64 lo = ~0ull, hi = 0;
+  s.entries([&](int token, float v) {
+    if (v > -INFINITY && in(v)) {
+      const u64 at = place_of(v, token);
+      lo = at < lo ? at : lo;
+      hi = at > hi ? at : hi;
+    }
   });
-  const Words ends = exchange(x, turn, parts, rank, g.lo, g.hi, Min(), Max());
+  const Words ends = exchange<Min, Max>(w.x, w.turn, w.parts, w.rank, lo, hi);
   g.lo = ends.a;
   g.hi = ends.b;
   while (g.count > most) {
-    const int bits = 64 - __clzll(static_cast<long long>(g.hi - g.lo)), shift = bits > 11 ? bits - 11 : 0;
-    clear_bins(h, by_mass);
-    s.sweep([&](int token, const auto& v) {
-#pragma unroll
-      for (int e = 0; e < S::E; ++e) {
-        const u64 at = place_of(v[e], token + e);
-        if (v[e] > -INFINITY && token + e >= 0 && at >= g.lo && at <= g.hi)
-          add_to_bin(h, static_cast<int>((g.hi - at) >> shift), by_mass, by_mass ? Weight::whole(w->of(v[e])) : 0);
+    const int bits = 64 - __clzll(static_cast<long long>(g.hi - g.lo)), shift = bits > kBinBits ? bits - kBinBits : 0;
+    __syncthreads();
+    clear_bins(w.h);
+    __syncthreads();
+    s.entries([&](int token, float v) {
+      const u64 at = place_of(v, token);
+      if (v > -INFINITY && at >= g.lo && at <= g.hi) {
+        const int bin = static_cast<int>((g.hi - at) >> shift);
+        atomicAdd(&w.h.count[bin], 1u);
+        if (by_mass) {  // 64 bits in two words: whoever makes the low one overflow carries
+          const u64 m = weight(v);
+          const unsigned was = atomicAdd(&w.h.lo[bin], static_cast<unsigned>(m));
+          const unsigned up = static_cast<unsigned>(m >> 32) + (was + static_cast<unsigned>(m) < was ? 1u : 0u);
+          if (up) atomicAdd(&w.h.hi[bin], up);
+        }
       }
     });
+    row_barrier(w.parts);
     Bins b;
-    merge_bins(h, x, turn, parts, rank, by_mass, b);
-    const Found sub = locate(h, b, parts, by_mass, target - (by_mass ? g.before_mass : g.before_count), slot);
-    slot ^= 1;
+    merge_bins(w, by_mass, by_mass, b, [](int, unsigned, u64 lo, unsigned hi) { return (static_cast<u64>(hi) << 32) + lo; });
+    const Found sub = locate(w, b, by_mass, target - (by_mass ? g.before_mass : g.before_count));
     g.before_count += sub.before_count;
     g.before_mass += sub.before_mass;
     g.count = sub.count;
@@ -292,65 +385,152 @@ __device__ __forceinline__ Range narrow(H& h, Exchange& x, int& turn, int& slot,
   return g;
 }
 
-// The last place of the line that is kept, by count (the first `target` tokens) or by mass (while what lies before is below `target`), given the bin that
-// `target` falls into; and the mass up to and with it.
-struct Limit {
-  u64 place, mass;
+// Sums of the first n threads' words before this one, in order of the threads, and over all of them; the other warps only come along.
+struct Scan {
+  u64 before, all;
 };
-template <class H, class S, class In>
-__device__ __forceinline__ Limit limit_in(H& h, Exchange& x, int& turn, int& slot, int parts, int rank, const S& s, const Weight& w, bool by_mass, bool masses, u64 target, const Found& f, In&& in) {
-  Range g = {0, 0, f.before_count, f.before_mass, f.count};
-  int n;
-  if (f.count <= kCandidates) {
-    n = gather(h, x, turn, parts, rank, s, in);
-  } else {
-    g = narrow(h, x, turn, slot, parts, rank, s, &w, by_mass, target, f, kCandidates, in);
-    // (masses before a range found by counts are not known: they are summed up where they are wanted)
-    n = gather(h, x, turn, parts, rank, s, [&](float v, int token) {
+template <class H>
+__device__ __forceinline__ Scan block_scan(H& h, int n, u64 mine) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = (n + 31) >> 5;
+  u64 up = mine;
+  if (warp < warps) {
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const u64 o = __shfl_up_sync(0xffffffffu, up, d);
+      if (lane >= d) up += o;
+    }
+    if (lane == 31) h.scan_mass[warp] = up;
+  }
+  __syncthreads();
+  Scan s = {up - mine, 0};
+  for (int i = 0; i < warps; ++i) {
+    const u64 o = h.scan_mass[i];
+    if (i < warp) s.before += o;
+    s.all += o;
+  }
+  __syncthreads();
+  return s;
+}
+
+// The first n threads' words, no two alike, in falling order (the other threads bring 0): thread i gets the i-th.  Few of them by counting, each by several lanes,
+// how many are larger; more of them by a bitonic network.
+template <class H>
+__device__ __forceinline__ u64 sorted(H& h, int n, u64 v) {
+  const int i = threadIdx.x;
+  if (n <= kFew) {
+    if (i < n) h.merged[i] = v;
+    __syncthreads();
+    const int wide = n > 1 ? 32 - __clz(n - 1) : 0, split = 9 - wide > 5 ? 5 : 9 - wide, lanes = 1 << split;  // 2^wide >= n candidates, 2^split lanes for each
+    const int of = i >> split;
+    const u64 mine = of < n ? h.merged[of] : 0;
+    int larger = 0;
+#pragma unroll 4
+    for (int j = i & (lanes - 1); j < n; j += lanes) larger += h.merged[j] > mine;
+    for (int d = 1; d < lanes; d *= 2) larger += __shfl_xor_sync(0xffffffffu, larger, d);
+    if (of < n && (i & (lanes - 1)) == 0) h.order[larger] = mine;
+    __syncthreads();
+    return i < n ? h.order[i] : 0;
+  }
+  const auto step = [&](u64 o, bool up) { return up ? Max::two(v, o) : Min::two(v, o); };
+#pragma unroll
+  for (int block = 2; block <= 32; block *= 2)
+#pragma unroll
+    for (int stride = block / 2; stride > 0; stride /= 2) v = step(__shfl_xor_sync(0xffffffffu, v, stride), ((i & stride) == 0) == ((i & block) == 0));
+#pragma unroll 1
+  for (int block = 64; block < 2 * n; block *= 2) {
+#pragma unroll 1
+    for (int stride = block >> 1; stride >= 32; stride >>= 1) {
+      __syncthreads();
+      h.merged[i] = v;
+      __syncthreads();
+      v = step(h.merged[i ^ stride], ((i & stride) == 0) == ((i & block) == 0));
+    }
+#pragma unroll
+    for (int stride = 16; stride > 0; stride /= 2) v = step(__shfl_xor_sync(0xffffffffu, v, stride), ((i & stride) == 0) == ((i & block) == 0));
+  }
+  return v;
+}
+
+// The n candidates of the row in order, one a thread: right behind taken().
+template <class H>
+__device__ __forceinline__ u64 in_order(Row<H>& w, int n) {
+  merge_lists(w, n);
+  return sorted(w.h, n, static_cast<int>(threadIdx.x) < n ? w.h.merged[threadIdx.x] : 0);  // (which this thread wrote)
+}
+// The place of the last thread of which `kept` holds: of the first ones, in order.
+template <class H>
+__device__ __forceinline__ u64 last_of(H& h, bool kept, u64 place) {
+  const int n = __syncthreads_count(kept);
+  if (static_cast<int>(threadIdx.x) == n - 1) h.word[0] = place;
+  __syncthreads();
+  const u64 at = h.word[0];
+  __syncthreads();
+  return at;
+}
+
+// The last place of the line that is kept by count: the first `target` tokens.
+template <class H, class S, class W, class BinOf>
+__device__ __forceinline__ u64 limit_by_count(Row<H>& w, const S& s, W&& weight, u64 target, const Found& f, BinOf&& bin_of) {
+  Range g = {0, ~0ull, f.before_count, 0, f.count};
+  if (f.count > kCandidates) g = narrow(w, s, weight, false, target, g, kCandidates, [&](float v) { return bin_of(v) == f.bin; });
+  s.entries([&](int token, float v) {
+    if (v > -INFINITY && bin_of(v) == f.bin) {
       const u64 at = place_of(v, token);
-      return v > -INFINITY && token >= 0 && at >= g.lo && at <= g.hi;
+      if (at >= g.lo && at <= g.hi) list(w.h, v, token);
+    }
+  });
+  const int n = static_cast<int>(taken(w).n);
+  const u64 place = in_order(w, n);
+  return last_of(w.h, static_cast<int>(threadIdx.x) < n && g.before_count + threadIdx.x < target, place);
+}
+
+// ... and by mass: those before which less than `target` lies, 1 <= target <= the mass of the row.  b: the row's bins, whose masses are estimates; bin_at: a
+// logit's bin before it is cut to a whole number.
+template <int DT, class H, class BinAt>
+__device__ __forceinline__ u64 limit_by_mass(Row<H>& w, const RowSlice<DT>& s, const Weight<DT>& weight, u64 target, const Bins& b, BinAt&& bin_at) {
+  const auto weigh = [&](float v) { return weight.of(v); };
+  Found f = locate(w, b, true, Max::two(1, Min::two(target, b.all_mass)));
+  Range g;
+  int n;
+  for (;;) {  // the estimates are good to 1e-4: the bin is this one or one next to it
+    const auto in = [&](float v) { return min(static_cast<int>(bin_at(v)), kBins - 1) == f.bin; };
+    const float lo = static_cast<float>(f.bin);
+    const bool few = f.count <= kCandidates;
+    u64 above = 0, inside = 0;
+    s.raw([&](int token, const uint4& r) {
+      above += weight.of_vector(r, token, [&](float v, int) { return bin_at(v) < lo; });
+#pragma unroll
+      for (int e = 0; e < Elem<DT>::E; ++e) {
+        const float v = entry<DT>(r, e);
+        if (v > -INFINITY && in(v)) {
+          inside += weigh(v);
+          if (few) list(w.h, v, token + e);
+        }
+      }
     });
-    if (masses && !by_mass) {
-      u64 sum = 0;
-      s.sweep([&](int token, const auto& v) {
-#pragma unroll
-        for (int e = 0; e < S::E; ++e)
-          if (v[e] > -INFINITY && token + e >= 0 && place_of(v[e], token + e) > g.hi) sum += Weight::whole(w.of(v[e]));
+    const Taken got = taken<Add, Add>(w, above, inside);
+    g = {0, ~0ull, f.before_count, got.sum, f.count};
+    n = static_cast<int>(got.n);
+    if (target <= got.sum && f.before_count > 0) {
+      f = locate(w, b, false, f.before_count);
+    } else if (target > got.sum + got.listed && f.before_count + f.count < b.all_count) {
+      f = locate(w, b, false, f.before_count + f.count + 1);
+    } else if (few) {
+      break;
+    } else {
+      g = narrow(w, s, weigh, true, target, g, kCandidates, in);
+      s.entries([&](int token, float v) {
+        const u64 at = place_of(v, token);
+        if (v > -INFINITY && at >= g.lo && at <= g.hi) list(w.h, v, token);
       });
-      g.before_mass = exchange(x, turn, parts, rank, sum, 0, Add(), Add()).a;
+      n = static_cast<int>(taken(w).n);
+      break;
     }
   }
-  const int i = threadIdx.x;  // (kCandidates == kSliceThreads)
-  const u64 mine = i < n ? h.merged[i] : 0;
-  const u64 weight = i < n && masses ? Weight::whole(w.of(logit_at(mine))) : 0;
-  h.mass[i] = weight;
-  __syncthreads();
-  u64 rank_of = g.before_count, mass = g.before_mass;
-  for (int j = 0; j < n; ++j)
-    if (h.merged[j] > mine) {
-      ++rank_of;
-      mass += h.mass[j];
-    }
-  // the tokens of the list that are kept: their last place, and the largest sum with one of them
-  const bool kept = i < n && (by_mass ? mass < target : rank_of < target);
-  u64 last = kept ? mine : ~0ull, sum = kept ? mass + weight : 0;
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) {
-    last = Min()(last, __shfl_xor_sync(0xffffffffu, last, d));
-    sum = Max()(sum, __shfl_xor_sync(0xffffffffu, sum, d));
-  }
-  if ((i & 31) == 0) {
-    h.scan_count[i >> 5] = last;
-    h.scan_mass[i >> 5] = sum;
-  }
-  __syncthreads();
-  Limit l = {~0ull, 0};
-  for (int k = 0; k < kSliceWarps; ++k) {
-    l.place = Min()(l.place, h.scan_count[k]);
-    l.mass = Max()(l.mass, h.scan_mass[k]);
-  }
-  __syncthreads();
-  return l;
+  const u64 place = in_order(w, n);
+  const bool there = static_cast<int>(threadIdx.x) < n;
+  const Scan up = block_scan(w.h, n, there ? weigh(logit_at(place)) : 0ull);
+  return last_of(w.h, there && g.before_mass + up.before < target, place);
 }
 
 // The row's entries that f(value, token) keeps, -inf in place of the others.
@@ -390,19 +570,72 @@ __device__ __forceinline__ void write_filtered(const RowSlice<DT>& s, char* row,
   }
 }
 
-// The largest entry (NaN where there is one) of the row, brought here on the way.
-template <int DT>
-__device__ __forceinline__ float load_max(const RowSlice<DT>& s, Exchange& x, int& turn, int parts, int rank) {
+// Behind start(): the row's largest entry (NaN where there is one), the smallest of its 512 groups' largest ones that are above -inf (the largest, where none is),
+// this lane's and this thread's group's.
+struct Groups {
+  float largest, smallest, own, group;
+};
+template <int DT, class H>
+__device__ __forceinline__ Groups group_max(Row<H>& w, const RowSlice<DT>& s) {
+  constexpr int E = Elem<DT>::E;
+  const int tid = threadIdx.x, lane = tid & 31;
+  Groups g;
+  s.finish();
   float m = -INFINITY;
-  s.load([&](const float (&v)[RowSlice<DT>::E]) {
+  s.vectors([&](int, const float (&v)[E]) {
 #pragma unroll
-    for (int e = 0; e < RowSlice<DT>::E; ++e) m = max_nan(m, v[e]);
+    for (int e = 0; e < E; ++e) m = max_nan(m, v[e]);
   });
-  if (parts > 1) cluster_barrier_wait();  // (every block of the row has started)
-  const auto larger = [](u64 a, u64 b) {
-    return static_cast<u64>(__float_as_uint(max_nan(__uint_as_float(static_cast<unsigned>(a)), __uint_as_float(static_cast<unsigned>(b)))));
-  };
-  return __uint_as_float(static_cast<unsigned>(exchange(x, turn, parts, rank, __float_as_uint(m), 0, larger, Max()).a));
+  g.own = m;
+  for (int d = 1; d < w.parts; d <<= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, d));
+  if (w.parts > 1) {
+    cluster_barrier_wait();  // (every block of the row has started)
+    const int to = tid & (w.parts - 1);
+    *of_rank(&w.h.group[(w.rank * kSliceThreads + tid) / w.parts], to) = m;
+  } else {
+    w.h.group[tid] = m;
+  }
+  row_barrier(w.parts);
+  g.group = w.h.group[tid];
+  const unsigned key = g.group != g.group ? 0xffffffffu : ordered(g.group);  // (NaN above all)
+  const unsigned hi = __reduce_max_sync(0xffffffffu, key), lo = __reduce_min_sync(0xffffffffu, g.group == -INFINITY ? 0xffffffffu : key);
+  if (lane == 0) {
+    w.h.scan_count[tid >> 5] = hi;
+    w.h.scan_mass[tid >> 5] = lo;
+  }
+  __syncthreads();
+  const unsigned top = __reduce_max_sync(0xffffffffu, static_cast<unsigned>(w.h.scan_count[lane & (kSliceWarps - 1)]));
+  const unsigned low = __reduce_min_sync(0xffffffffu, static_cast<unsigned>(w.h.scan_mass[lane & (kSliceWarps - 1)]));
+  g.largest = top == 0xffffffffu ? __int_as_float(0x7fc00000) : unordered(top);
+  g.smallest = low == 0xffffffffu ? g.largest : unordered(low);
+  return g;  // (the two arrays are written next behind a barrier of the block)
+}
+
+// A logit that at least k of the groups reach, the largest one up to 1/64 of the range that the groups' largest logits span; -inf where fewer groups have a token.
+// h.steps is 0, and is again.
+template <class H>
+__device__ __forceinline__ float reached_by(H& h, const Groups& g, int k) {
+  const int tid = threadIdx.x, lane = tid & 31;
+  const float span = g.largest - g.smallest, per = 64.0f / span;  // (span: overflows to inf for logits further apart than floats go: all in the first step)
+  if (g.group > -INFINITY) atomicAdd(&h.steps[min(static_cast<int>((g.largest - g.group) * per), 63)], 1u);
+  __syncthreads();
+  const unsigned a = h.steps[2 * lane], b = h.steps[2 * lane + 1];
+  unsigned up = a + b;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const unsigned o = __shfl_up_sync(0xffffffffu, up, d);
+    if (lane >= d) up += o;
+  }
+  const unsigned enough = __ballot_sync(0xffffffffu, up >= static_cast<unsigned>(k));
+  const int first = enough ? __ffs(enough) - 1 : 31;
+  const bool lower = __shfl_sync(0xffffffffu, up - b, first) >= static_cast<unsigned>(k);
+  const int step = 2 * first + (lower ? 1 : 2);
+  __syncthreads();
+  if (tid < 64) h.steps[tid] = 0;
+  if (!enough) return -INFINITY;
+  if (step >= 64 || !(span > 0.0f && span < INFINITY)) return g.smallest;
+  // (a hundredth of a step for the rounding of the steps)
+  return __double2float_rd(static_cast<double>(g.largest) - (static_cast<double>(step) + 0.01) * static_cast<double>(span) / 64.0);
 }
 
 template <int DT>
@@ -410,16 +643,25 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
   extern __shared__ uint4 smem[];
   SampleShared& h = *reinterpret_cast<SampleShared*>(smem);
   __shared__ Exchange x;
-  __shared__ double table[64];
+  __shared__ double table[kTable];
   const int parts = p.c.parts, rank = blockIdx.x % parts, row = blockIdx.x / parts, tid = threadIdx.x;
   if (parts > 1) cluster_barrier_arrive();
-  int turn = 0, slot = 0;
-  if (tid < 64) table[tid] = exp2(static_cast<double>(tid) / 64.0);
+  wait_for_inputs();
   RowSlice<DT> s;
   s.init(static_cast<const char*>(p.c.logits) + static_cast<long long>(row) * p.c.stride * Elem<DT>::bytes, p.c.V, rank, p.c.share, p.c.seg, smem + sizeof(h) / 16, p.c.res);
+  s.start();
   const float T = p.row_T ? p.row_T[row] : p.T;
-  const float m = load_max(s, x, turn, parts, rank);
+  int k = p.row_k ? p.row_k[row] : p.k;
+  const float top_p = p.row_p ? p.row_p[row] : p.p, min_p = p.row_min_p ? p.row_min_p[row] : p.min_p;
+  const double u = fmin(fmax(static_cast<double>(p.u[row]), 0.0), 1.0);  // (NaN: 0)
   char* const filtered = p.filtered ? p.filtered + static_cast<long long>(row) * p.stride_filtered * Elem<DT>::bytes : nullptr;
+  table[tid] = exp2(static_cast<double>(tid) / kTable);
+  clear_bins(h);
+  if (tid < 64) h.steps[tid] = 0;
+  if (tid == 0) h.listed = 0;
+  Row<SampleShared> w = {h, x, parts, rank, 0, 0};
+  const Groups groups = group_max(w, s);
+  const float m = groups.largest, own = groups.own;
 
   if (!(m > -INFINITY && m < INFINITY) || !(T >= 0.0f)) {
     if (rank == 0 && tid == 0) {
@@ -434,12 +676,10 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
 
   if (T == 0.0f) {
     u64 first = ~0ull;
-    s.sweep([&](int token, const auto& v) {
-#pragma unroll
-      for (int e = 0; e < RowSlice<DT>::E; ++e)
-        if (v[e] == m && static_cast<u64>(token + e) < first) first = static_cast<u64>(token + e);
+    s.entries([&](int token, float v) {
+      if (v == m) first = Min::two(first, static_cast<u64>(token));
     });
-    const int token = static_cast<int>(exchange(x, turn, parts, rank, first, 0, Min(), Max()).a);
+    const int token = static_cast<int>(exchange<Min>(x, w.turn, parts, rank, first).a);
     if (rank == 0 && tid == 0) {
       p.tokens[row] = token;
       if (p.prob) p.prob[row] = 1.0f;
@@ -450,112 +690,181 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
     return;
   }
 
-  int k = p.row_k ? p.row_k[row] : p.k;
   if (k <= 0 || k > p.c.V) k = p.c.V;
-  const float top_p = p.row_p ? p.row_p[row] : p.p, min_raw = p.row_min_p ? p.row_min_p[row] : p.min_p;
-  const bool by_p = top_p < 1.0f;
-  Weight w = {static_cast<double>(m), 1.4426950408889634 / static_cast<double>(T), table, min(46, 63 - (32 - __clz(p.c.V - 1)))};
-  const double least = ldexp(min_raw > 0.0f ? fmin(static_cast<double>(min_raw), 1.0) : 0.0, w.scale);
+  const bool by_k = k < p.c.V, by_p = top_p < 1.0f;
+  Weight<DT> weight;
+  weight.init(m, T, p.c.V, table);
+  const auto weigh = [&](float v) { return weight.of(v); };
+  // min-p as a logit: w >= min_p where l >= m + T ln(min_p)
+  const float least = min_p > 0.0f ? __double2float_ru(fma(static_cast<double>(T), log(fmin(static_cast<double>(min_p), 1.0)), static_cast<double>(m))) : -INFINITY;
+  const auto share_of = [&](u64 mass) {  // of top-p: at least a unit, so that the first token is kept
+    const double want = ceil(static_cast<double>(fmaxf(top_p, 0.0f)) * static_cast<double>(mass));
+    return want < 1.0 ? 1ull : static_cast<u64>(want);
+  };
+  const auto drawn = [&](u64 mass) {  // the unit of mass that u falls on
+    const double want = ceil(u * static_cast<double>(mass));
+    return want >= static_cast<double>(mass) ? mass : (want < 1.0 ? 1ull : static_cast<u64>(want));
+  };
 
-  // the last place that is kept; nothing at -inf is
-  u64 last = static_cast<u64>(ordered(-INFINITY) + 1) << 32;
-  if (k < p.c.V || by_p) {
+  u64 last = place_of(-3.402823466e+38f, 0x7fffffff);  // the last place that is kept; nothing at -inf is
+  if (by_k || by_p) {
     // bins of 1/32 of a power of two of the weight where sums of weights are wanted, else of 1/64 of a logit
-    const float per = by_p ? fminf(46.166241f / T, 1e30f) : 64.0f;
-    const auto bin_of = [&](float v) { return min(static_cast<int>((m - v) * per), kBins - 1); };
-    clear_bins(h, by_p);
-    s.sweep([&](int, const auto& v) {
+    const float per_half = by_p ? fminf(32.0f * weight.c32x2, 1e30f) : 128.0f;
+    const auto bin_at = [&](float v) { return fmaf(-0.5f, v, weight.half) * per_half; };
+    const auto bin_of = [&](float v) { return min(static_cast<int>(bin_at(v)), kBins - 1); };
+    const auto count_in = [&](float v) {
+      if (v > -INFINITY) {
+        const float at = bin_at(v);
+        const int bin = min(static_cast<int>(at), kBins - 1);
+        atomicAdd(&h.count[bin], 1u);
+        if (by_p && bin < kBins - 1) atomicAdd(&h.lo[bin], static_cast<unsigned>((at - static_cast<float>(bin)) * 16.0f));
+      }
+    };
+    u64 total = 0;  // what top-p is a part of
+    bool counted = false;
+    if (!by_k || k <= kHeadMost) {
+      const float from = reached_by(h, groups, by_k ? k : min(kHeadGuess, p.c.V));
+      u64 sum = 0, mass = 0;
+      if (!by_k) {  // (everything is looked at for the total; the histogram is filled on the way, for rows that want it)
+        s.raw([&](int token, const uint4& r) {
+          sum += weight.of_vector(r, token, [](float, int) { return true; });
 #pragma unroll
-      for (int e = 0; e < RowSlice<DT>::E; ++e)
-        if (v[e] > -INFINITY) add_to_bin(h, bin_of(v[e]), by_p, by_p ? Weight::whole(w.of(v[e])) : 0);
-    });
+          for (int e = 0; e < Elem<DT>::E; ++e) {
+            const float v = entry<DT>(r, e);
+            count_in(v);
+            if (v >= from && v > -INFINITY) {
+              mass += weigh(v);
+              list(h, v, token + e);
+            }
+          }
+        });
+        counted = true;
+      } else if (own >= from) {
+        s.entries([&](int token, float v) {
+          if (v >= from && v > -INFINITY) list(h, v, token);
+        });
+      }
+      const Taken got = taken<Add, Add>(w, sum, mass);
+      total = got.sum;
+      const u64 part = by_k ? 0 : share_of(total);
+      if (got.n <= kCandidates && got.listed >= part) {  // the limits lie among these
+        const int n = static_cast<int>(got.n);
+        const u64 place = in_order(w, n);
+        const bool there = tid < n && tid < k;
+        const float logit = logit_at(place);
+        const u64 mine = there ? weigh(logit) : 0;
+        const Scan up = block_scan(h, n, mine);
+        const u64 target = by_k ? (by_p ? share_of(up.all) : ~0ull) : part;
+        const bool kept = there && up.before < target && logit >= least;
+        const int count = __syncthreads_count(kept);
+        if (tid == count - 1) {
+          h.word[0] = place;
+          h.word[1] = up.before + mine;
+        }
+        __syncthreads();
+        last = h.word[0];
+        const u64 all = h.word[1];
+        if (rank == 0) {
+          // in order of the index
+          const u64 by_token = sorted(h, count, kept ? ~(static_cast<u64>(token_at(place)) << 32 | place >> 32) : 0);
+          const bool of_these = tid < count;
+          const float l = unordered(~static_cast<unsigned>(by_token));
+          const u64 weighs = of_these ? weigh(l) : 0, goal = drawn(all);
+          const u64 before = block_scan(h, count, weighs).before;
+          if (of_these && before < goal && goal <= before + weighs) {
+            p.tokens[row] = static_cast<int>(~static_cast<unsigned>(by_token >> 32));
+            if (p.prob) p.prob[row] = static_cast<float>(weight.exact(l) / static_cast<double>(all));
+          }
+          if (tid == 0) {
+            if (p.kept) p.kept[row] = count;
+            if (p.status) p.status[row] = 0;
+          }
+        }
+        if (filtered) write_filtered<DT>(s, filtered, [&](float v, int token) { return v > -INFINITY && place_of(v, token) >= last; });
+        row_barrier(parts);  // (no block leaves while another reads its list)
+        return;
+      }
+    }
+    if (!counted) {
+      s.entries([&](int, float v) { count_in(v); });
+      row_barrier(parts);
+    }
     Bins b;
-    merge_bins(h, x, turn, parts, rank, by_p, b);
-    u64 mass = b.all_mass;
-    if (static_cast<u64>(k) < b.all_count) {
-      const Found f = locate(h, b, parts, false, k, slot);
-      slot ^= 1;
-      const Limit l = limit_in(h, x, turn, slot, parts, rank, s, w, false, by_p, k, f, [&](float v, int) { return v > -INFINITY && bin_of(v) == f.bin; });
-      last = l.place;
-      mass = l.mass;
+    // the weights of a bin, from the places of its tokens in it (in sixteenths), up to the curvature of exp2 over it (6e-5)
+    merge_bins(w, by_p, false, b, [&](int bin, unsigned count, u64 sixteenths, unsigned) {
+      const float part = static_cast<float>(count) - 0.00133925f * (static_cast<float>(sixteenths) + 0.5f * static_cast<float>(count));  // (1 - 2^(-1/32)) / 16
+      return bin == kBins - 1 ? 0ull : static_cast<u64>(weight.power(-bin * (kTable / 32)) * static_cast<double>(part));
+    });
+    if (by_k && static_cast<u64>(k) < b.all_count) {
+      const Found f = locate(w, b, false, k);
+      last = limit_by_count(w, s, weigh, k, f, bin_of);
     }
     if (by_p) {
-      const double want = ceil(static_cast<double>(fmaxf(top_p, 0.0f)) * static_cast<double>(mass));
-      u64 target = want < 1.0 ? 1 : static_cast<u64>(want);  // (the first one is kept in any case; NaN counts as no limit above)
-      if (target < mass) {
-        const Found f = locate(h, b, parts, true, target, slot);
-        slot ^= 1;
-        const Limit l = limit_in(h, x, turn, slot, parts, rank, s, w, true, true, target, f, [&](float v, int) { return v > -INFINITY && bin_of(v) == f.bin; });
-        last = Max()(last, l.place);
+      if (by_k) {
+        u64 mine = 0;
+        s.raw([&](int token, const uint4& r) {
+          mine += weight.of_vector(r, token, [&](float v, int t) { return v > -INFINITY && place_of(v, t) >= last; });
+        });
+        total = exchange<Add>(x, w.turn, parts, rank, mine).a;
       }
+      const u64 target = share_of(total);
+      if (target < total) last = Max::two(last, limit_by_mass<DT>(w, s, weight, target, b, bin_at));
     }
   }
 
   // what is kept, in order of the index
-  const auto keeps = [&](float v, int token) { return place_of(v, token) >= last && v > -INFINITY; };
+  const float last_logit = logit_at(last);
+  const int last_token = token_at(last);
+  const auto keeps = [&](float v, int token) { return v >= least && v >= last_logit && (v > last_logit || token <= last_token); };
   u64 mine = 0, kept = 0;
-  s.sweep([&](int token, const auto& v) {
-#pragma unroll
-    for (int e = 0; e < RowSlice<DT>::E; ++e)
-      if (keeps(v[e], token + e)) {
-        const double we = w.of(v[e]);
-        if (we >= least) {
-          mine += Weight::whole(we);
-          ++kept;
-        }
-      }
-  });
-  const int t = turn & 1;
-  const Words all = exchange(x, turn, parts, rank, mine, kept, Add(), Add());
-  const double u = static_cast<double>(p.u[row]);
-  const double want = ceil(fmin(fmax(u, 0.0), 1.0) * static_cast<double>(all.a));
-  const u64 target = want >= static_cast<double>(all.a) ? all.a : (want < 1.0 ? 1 : static_cast<u64>(want));
+  if (own >= fmaxf(least, last_logit))
+    s.raw([&](int token, const uint4& r) {
+      mine += weight.of_vector(r, token, [&](float v, int t) {
+        const bool it = keeps(v, t);
+        kept += it;
+        return it;
+      });
+    });
+  const int t = w.turn & 1;
+  const Words all = exchange<Add, Add>(x, w.turn, parts, rank, mine, kept);
+  const u64 goal = drawn(all.a);
   u64 before = 0;
   for (int r = 0; r < rank; ++r) before += x.a[t][r];
-  if (before < target && target <= before + x.a[t][rank]) {
+  if (before < goal && goal <= before + x.a[t][rank]) {
     const int lane = tid & 31, warp = tid >> 5;
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d);
+    mine = Add::warp(mine);
     if (lane == 0) h.scan_mass[warp] = mine;
     __syncthreads();
     for (int i = 0; i < warp; ++i) before += h.scan_mass[i];
-    if (before < target && target <= before + mine) {  // this warp has it
-      const int steps = (s.end - s.begin + 31) / 32;
-      for (int q = 0; q < steps; ++q) {
-        const int i = s.begin + q * 32 + lane;
+    if (before < goal && goal <= before + mine) {  // this warp has it
+      for (int at = s.begin; at < s.end; at += 32) {
+        const int i = at + lane;
         const uint4 r = i < s.end ? s.at(i) : neg_inf_vector<DT>();
-        float v[RowSlice<DT>::E];
-        Elem<DT>::unpack(r, v);
         const int token = s.token(i);
-        u64 sum = 0;
-#pragma unroll
-        for (int e = 0; e < RowSlice<DT>::E; ++e)
-          if (keeps(v[e], token + e)) {
-            const double we = w.of(v[e]);
-            if (we >= least) sum += Weight::whole(we);
-          }
+        const u64 sum = weight.of_vector(r, token, keeps);
         u64 up = sum;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
           const u64 o = __shfl_up_sync(0xffffffffu, up, d);
           if (lane >= d) up += o;
         }
-        const unsigned reached = __ballot_sync(0xffffffffu, before + up >= target);
+        const unsigned reached = __ballot_sync(0xffffffffu, before + up >= goal);
         if (reached) {
           if (lane == __ffs(reached) - 1) {
-            u64 at = before + up - sum;
+            before += up - sum;
             bool open = true;
 #pragma unroll
-            for (int e = 0; e < RowSlice<DT>::E; ++e)
-              if (open && keeps(v[e], token + e)) {
-                const double we = w.of(v[e]);
-                if (we >= least) at += Weight::whole(we);
-                if (we >= least && at >= target) {
+            for (int e = 0; e < RowSlice<DT>::E; ++e) {
+              const float v = entry<DT>(r, e);
+              if (open && keeps(v, token + e)) {
+                before += weigh(v);
+                if (before >= goal) {
                   open = false;
                   p.tokens[row] = token + e;
-                  if (p.prob) p.prob[row] = static_cast<float>(we / static_cast<double>(all.a));
+                  if (p.prob) p.prob[row] = static_cast<float>(weight.exact(v) / static_cast<double>(all.a));
                 }
               }
+            }
           }
           break;
         }
@@ -567,23 +876,25 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
     if (p.kept) p.kept[row] = static_cast<int>(all.b);
     if (p.status) p.status[row] = 0;
   }
-  if (filtered) {
-    // (the weight is at the minimum or above it: tested by it where the two are close, since the logits of the type are)
-    write_filtered<DT>(s, filtered, [&](float v, int token) { return keeps(v, token) && (least == 0.0 || w.of(v) >= least); });
-  }
+  if (filtered) write_filtered<DT>(s, filtered, keeps);
 }
 
-template <int DT>
-__global__ void __launch_bounds__(kSliceThreads, 2) cos_top_kernel(const TopParams p) {
+template <int DT, int kList>
+__global__ void __launch_bounds__(kSliceThreads, 3) cos_top_kernel(const TopParams p) {
   extern __shared__ uint4 smem[];
-  TopShared& h = *reinterpret_cast<TopShared*>(smem);
+  Shared<kList>& h = *reinterpret_cast<Shared<kList>*>(smem);
   __shared__ Exchange x;
   const int parts = p.c.parts, rank = blockIdx.x % parts, row = blockIdx.x / parts, tid = threadIdx.x;
   if (parts > 1) cluster_barrier_arrive();
-  int turn = 0, slot = 0;
+  wait_for_inputs();
   RowSlice<DT> s;
   s.init(static_cast<const char*>(p.c.logits) + static_cast<long long>(row) * p.c.stride * Elem<DT>::bytes, p.c.V, rank, p.c.share, p.c.seg, smem + sizeof(h) / 16, p.c.res);
-  const float m = load_max(s, x, turn, parts, rank);
+  s.start();
+  if (tid < 64) h.steps[tid] = 0;
+  if (tid == 0) h.listed = 0;
+  Row<Shared<kList>> w = {h, x, parts, rank, 0, 0};
+  const Groups groups = group_max(w, s);
+  const float m = groups.largest, own = groups.own;
   float* const values = p.values + static_cast<long long>(row) * p.k;
   int* const ids = p.ids + static_cast<long long>(row) * p.k;
   if (!(m > -INFINITY && m < INFINITY)) {
@@ -596,47 +907,77 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_top_kernel(const TopPara
     }
     return;
   }
-  const auto bin_of = [&](float v) { return min(static_cast<int>((m - v) * 64.0f), kBins - 1); };
   const float c = fminf(static_cast<float>(1.4426950408889634 / static_cast<double>(p.T)), 3e38f);
-  clear_bins(h, false);
   double sum = 0.0;
-  s.sweep([&](int, const auto& v) {
+  s.vectors([&](int, const float (&v)[RowSlice<DT>::E]) {
     float part = 0.0f;  // (of a vector: eight terms of at most 1)
 #pragma unroll
-    for (int e = 0; e < RowSlice<DT>::E; ++e)
-      if (v[e] > -INFINITY) {
-        part += ex2_approx((v[e] - m) * c);
-        add_to_bin(h, bin_of(v[e]), false, 0);
-      }
+    for (int e = 0; e < RowSlice<DT>::E; ++e) part += ex2_approx((v[e] - m) * c);
     sum += static_cast<double>(part);
   });
-  const auto add = [](u64 a, u64 b) {
-    return static_cast<u64>(__double_as_longlong(__longlong_as_double(static_cast<long long>(a)) + __longlong_as_double(static_cast<long long>(b))));
-  };
-  const Words sums = exchange(x, turn, parts, rank, static_cast<u64>(__double_as_longlong(sum)), 0, add, Max());
-  if (rank == 0 && tid == 0)
-    p.lse[row] = static_cast<float>(static_cast<double>(m) / static_cast<double>(p.T) + log(__longlong_as_double(static_cast<long long>(sums.a))));
-  Bins b;
-  merge_bins(h, x, turn, parts, rank, false, b);
-  int n;
-  if (static_cast<u64>(p.k) < b.all_count) {
-    const Found f = locate(h, b, parts, false, p.k, slot);
-    slot ^= 1;
-    if (f.before_count + f.count <= kTopCandidates) {
-      n = gather(h, x, turn, parts, rank, s, [&](float v, int) { return v > -INFINITY && bin_of(v) <= f.bin; });
-    } else {
-      const Range g = narrow(h, x, turn, slot, parts, rank, s, static_cast<const Weight*>(nullptr), false, p.k, f, kTopCandidates - COS_TOP_MAX,
-                             [&](float v, int) { return v > -INFINITY && bin_of(v) == f.bin; });
-      n = gather(h, x, turn, parts, rank, s, [&](float v, int token) { return v > -INFINITY && token >= 0 && place_of(v, token) >= g.lo; });
-    }
+  int n = kList + 1;
+  if (p.k <= kHeadMost) {
+    const float from = reached_by(h, groups, p.k);
+    if (own >= from)
+      s.entries([&](int token, float v) {
+        if (v >= from && v > -INFINITY) list(h, v, token);
+      });
+    const Taken got = taken<AddDouble>(w, bits_of(sum));
+    n = static_cast<int>(got.n);
+    sum = double_of(got.sum);
   } else {
-    n = gather(h, x, turn, parts, rank, s, [&](float v, int) { return v > -INFINITY; });
+    sum = double_of(exchange<AddDouble>(x, w.turn, parts, rank, bits_of(sum)).a);
   }
-  for (int i = rank * kSliceThreads + tid; i < n; i += parts * kSliceThreads) {
-    const u64 mine = h.merged[i];
+  if (rank == 0 && tid == 0) p.lse[row] = static_cast<float>(static_cast<double>(m) / static_cast<double>(p.T) + log(sum));
+  if (n > kList) {
+    const auto bin_of = [&](float v) { return min(static_cast<int>(fmaf(-0.5f, v, 0.5f * m) * 128.0f), kBins - 1); };
+    clear_bins(h);
+    __syncthreads();
+    s.entries([&](int, float v) {
+      if (v > -INFINITY) atomicAdd(&h.count[bin_of(v)], 1u);
+    });
+    row_barrier(parts);
+    Bins b;
+    merge_bins(w, false, false, b, [](int, unsigned, u64, unsigned) { return 0ull; });
+    u64 from = 0;  // of places
+    if (static_cast<u64>(p.k) < b.all_count) {
+      const Found f = locate(w, b, false, p.k);
+      Range g = {0, 0, f.before_count, 0, f.count};
+      // (what lies before the bin is less than k, and kList holds as many and the rest)
+      if (f.before_count + f.count > kList) {
+        g = narrow(w, s, [](float) { return 0ull; }, false, p.k, g, kList - kMost<kList>, [&](float v) { return bin_of(v) == f.bin; });
+        from = g.lo;
+        s.entries([&](int token, float v) {
+          if (v > -INFINITY && place_of(v, token) >= from) list(h, v, token);
+        });
+      } else {
+        s.entries([&](int token, float v) {
+          if (v > -INFINITY && bin_of(v) <= f.bin) list(h, v, token);
+        });
+      }
+    } else {
+      s.entries([&](int token, float v) {
+        if (v > -INFINITY) list(h, v, token);
+      });
+    }
+    n = static_cast<int>(taken(w).n);
+  }
+  merge_lists(w, n);
+  __syncthreads();
+  // every block compares its share of the candidates with all of them, a candidate by as many lanes as there are
+  const int each = (n + parts - 1) / parts, end = min(n, (rank + 1) * each);
+  int lanes = 1;
+  while (lanes < 32 && 2 * lanes * each <= kSliceThreads) lanes *= 2;
+  for (int first = rank * each; first < end; first += kSliceThreads / lanes) {  // (the same for all lanes of a warp)
+    const int i = first + tid / lanes;
+    const u64 mine = i < end ? h.merged[i] : 0;
     int at = 0;
-    for (int j = 0; j < n; ++j) at += h.merged[j] > mine;
-    if (at < p.k) {
+    if (i < end) {
+#pragma unroll 4
+      for (int j = tid & (lanes - 1); j < n; j += lanes) at += h.merged[j] > mine;
+    }
+    for (int d = 1; d < lanes; d *= 2) at += __shfl_xor_sync(0xffffffffu, at, d);
+    if (i < end && (tid & (lanes - 1)) == 0 && at < p.k) {
       values[at] = logit_at(mine);
       ids[at] = token_at(mine);
     }
@@ -664,7 +1005,7 @@ cos_status launch_rows(P& p, int rows, int vocab, int dtype, int device, size_t 
   OnDevice on(device);
   if (on.error != cudaSuccess) return call_failed("cudaSetDevice", on.error);
   SlicePlan plan;
-  cudaError_t e = slice_plan(device, rows, vocab, dtype, &plan);
+  cudaError_t e = slice_plan(device, rows, vocab, dtype, 44 * 1024, true, &plan);
   if (e != cudaSuccess) return call_failed("device query", e);
   if (static_cast<long long>(rows) * plan.parts > 0x7fffffffll) return call_failed(COS_ERR_UNSUPPORTED, "too many rows for one launch");
   p.c.V = vocab;
@@ -680,19 +1021,17 @@ bool misaligned4(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 != 0
 
 }  // namespace
 
-cudaError_t slice_plan(int device, int rows, int vocab, int dtype, SlicePlan* plan) {
-  int sms = 0;
-  const cudaError_t e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+cudaError_t slice_plan(int device, int rows, int vocab, int dtype, int most, bool cluster, SlicePlan* plan) {
+  const cudaError_t e = cudaDeviceGetAttribute(&plan->sms, cudaDevAttrMultiProcessorCount, device);
   if (e != cudaSuccess) return e;
-  constexpr long long kMostKept = 64 * 1024 / 16;  // vectors: two blocks of a multiprocessor have room for that beside their histograms
-  const int E = dtype == COS_DTYPE_F32 ? 4 : 8;
+  const int E = dtype == COS_DTYPE_F32 ? 4 : 8, kept = most / 16;
   const long long all = (static_cast<long long>(vocab) + 2 * (E - 1)) / E;
-  int parts = 1;
-  while (parts < kSliceParts && ((all + parts - 1) / parts > kMostKept || (static_cast<long long>(rows) * parts < 2 * sms && all / parts >= 512))) parts *= 2;
-  plan->parts = parts;
+  long long parts = 1;
+  while ((parts < kSliceParts || !cluster) && ((all + parts - 1) / parts > kept || (rows * parts < 2 * plan->sms && all / parts >= kSliceThreads))) parts *= 2;
+  plan->parts = static_cast<int>(parts);
   plan->share = static_cast<int>((all + parts - 1) / parts);
   plan->seg = static_cast<int>((plan->share + 32 * kSliceWarps - 1) / (32 * kSliceWarps) * 32);
-  plan->res = static_cast<int>(plan->share < kMostKept ? plan->share : kMostKept);
+  plan->res = plan->share < kept ? plan->share : kept;
   plan->smem = static_cast<size_t>(plan->res) * 16;
   return cudaSuccess;
 }
@@ -757,7 +1096,11 @@ extern "C" cos_status cos_top_logits(const cos_top_args* a, void* cuda_stream) {
   p.values = a->values;
   p.ids = a->ids;
   p.lse = a->lse;
-  return launch_rows(p, a->rows, a->vocab, a->dtype, a->device, sizeof(TopShared), static_cast<cudaStream_t>(cuda_stream), [](int dt) {
-    return dt == COS_DTYPE_F32 ? cos_top_kernel<COS_DTYPE_F32> : (dt == COS_DTYPE_BF16 ? cos_top_kernel<COS_DTYPE_BF16> : cos_top_kernel<COS_DTYPE_F16>);
-  });
+  const auto call = [&](auto list) {
+    constexpr int kList = decltype(list)::value;
+    return launch_rows(p, a->rows, a->vocab, a->dtype, a->device, sizeof(Shared<kList>), static_cast<cudaStream_t>(cuda_stream), [](int dt) {
+      return dt == COS_DTYPE_F32 ? cos_top_kernel<COS_DTYPE_F32, kList> : (dt == COS_DTYPE_BF16 ? cos_top_kernel<COS_DTYPE_BF16, kList> : cos_top_kernel<COS_DTYPE_F16, kList>);
+    });
+  };
+  return a->k <= kMost<kCandidates> ? call(std::integral_constant<int, kCandidates>()) : call(std::integral_constant<int, kTopCandidates>());
 }

@@ -7,6 +7,8 @@
 #ifndef COS_SLICE_CUH
 #define COS_SLICE_CUH
 
+#include <type_traits>
+
 #include "cos_common.cuh"
 #include "cos_draft.h"
 
@@ -25,7 +27,7 @@ struct RowSlice {
   uint4* kept;       // the first `res` are here
   int res;
 
-  // part of `parts` vectors each, parts / 16 warps' worth (a multiple of 32)
+  // `share` vectors for each block, `seg` of them for each warp (a multiple of 32)
   __device__ __forceinline__ void init(const void* row, int V_, int rank, int share, int seg, uint4* smem, int res_) {
     const unsigned long long at = reinterpret_cast<unsigned long long>(row);
     base = reinterpret_cast<const char*>(at & ~15ull);
@@ -68,27 +70,27 @@ struct RowSlice {
   }
   __device__ __forceinline__ uint4 at(int i) const { return i < res ? kept[i] : fetch(i); }
 
-  // Brings the warp's part here; f(values) sees every vector on the way.
-  template <class F>
-  __device__ __forceinline__ void load(F&& f) const {
-    constexpr int kAhead = 4;
-    const int lane = threadIdx.x & 31;
-    for (int i = begin + lane; i < end; i += 32 * kAhead) {
-      uint4 r[kAhead];
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k) r[k] = i + 32 * k < end ? fetch(i + 32 * k) : neg_inf_vector<DT>();
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        if (i + 32 * k < end && i + 32 * k < res) kept[i + 32 * k] = r[k];
-        float v[E];
-        Elem<DT>::unpack(r[k], v);
-        f(v);
+  // Begins to bring the warp's part here: asynchronous copies, all of a lane's under way at once.  finish() waits for them (a lane reads only what it copied
+  // itself, so no barrier is needed).
+  __device__ __forceinline__ void start() const {
+    const int last = min(end, res);
+    for (int i = begin + (threadIdx.x & 31); i < last; i += 32) {
+      const int x = token(i);
+      const char* from = base + (static_cast<long long>(v0) + i) * 16;
+      if (x >= 0 && x <= V - E) {
+        const unsigned to = static_cast<unsigned>(__cvta_generic_to_shared(kept + i));
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+      } else {
+        kept[i] = ragged(from, x);
       }
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
   }
+  __device__ __forceinline__ void finish() const { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
   // f(token of the first entry, values) for every vector of this lane.
   template <class F>
-  __device__ __forceinline__ void sweep(F&& f) const {
+  __device__ __forceinline__ void vectors(F&& f) const {
     for (int i = begin + (threadIdx.x & 31); i < end; i += 32) {
       const uint4 r = at(i);
       float v[E];
@@ -96,7 +98,31 @@ struct RowSlice {
       f(token(i), v);
     }
   }
+  // f(token of the first entry, vector) likewise.
+  template <class F>
+  __device__ __forceinline__ void raw(F&& f) const {
+    for (int i = begin + (threadIdx.x & 31); i < end; i += 32) f(token(i), at(i));
+  }
+  // f(token, value) for every entry of this lane.  Two words of a vector at a time: a long body in eight copies is more instructions than are fetched in the time they take.
+  template <class F>
+  __device__ __forceinline__ void entries(F&& f) const {
+    for (int i = begin + (threadIdx.x & 31); i < end; i += 32) {
+      uint4 r = at(i);
+      int x = token(i);
+#pragma unroll 1
+      for (int q = 0; q < 2; ++q) {
+#pragma unroll
+        for (int e = 0; e < E / 2; ++e) f(x + e, entry<DT>(r, e));
+        r.x = r.z;
+        r.y = r.w;
+        x += E / 2;
+      }
+    }
+  }
 };
+
+// Everything that the work ahead in the stream wrote is there (launches take their places while it drains).
+__device__ __forceinline__ void wait_for_inputs() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // ------------------------------------------------------------------------------------
 // the cluster
@@ -105,6 +131,7 @@ __device__ __forceinline__ void cluster_barrier_arrive() { asm volatile("barrier
 __device__ __forceinline__ void cluster_barrier_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void row_barrier(int parts) {
   if (parts > 1) {
+    __syncwarp();
     cluster_barrier_arrive();
     cluster_barrier_wait();
   } else {
@@ -122,65 +149,127 @@ __device__ __forceinline__ float max_nan(float a, float b) {  // NaN where one i
   return r;
 }
 
-// Two words from every block of the row.  Used in turns: a block may write the next exchange while another still reads this one, not the one after
+// How a word is reduced over a warp and over a few words.  (Reductions of 32 bits in one instruction where they do: a shuffle is one for each warp and clock of the
+// whole multiprocessor, so 64-bit words by shuffles take 16 warps 500 clocks a word.)
+struct Add {  // below 2^64
+  using OfBlocks = Add;
+  static __device__ __forceinline__ u64 two(u64 a, u64 b) { return a + b; }
+  static __device__ __forceinline__ u64 warp(u64 v) {
+    const u64 lo = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(v) & 0xffffffu);
+    const u64 mid = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(v >> 24) & 0xffffffu);
+    const u64 hi = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(v >> 48));
+    return lo + (mid << 24) + (hi << 48);
+  }
+  static constexpr u64 none = 0;
+};
+struct AddDouble {
+  using OfBlocks = AddDouble;
+  static __device__ __forceinline__ u64 two(u64 a, u64 b) {
+    return static_cast<u64>(__double_as_longlong(__longlong_as_double(static_cast<long long>(a)) + __longlong_as_double(static_cast<long long>(b))));
+  }
+  static __device__ __forceinline__ u64 warp(u64 v) {
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) v = two(v, __shfl_xor_sync(0xffffffffu, v, d));
+    return v;
+  }
+  static constexpr u64 none = 0;
+};
+struct Max {
+  using OfBlocks = Max;
+  static __device__ __forceinline__ u64 two(u64 a, u64 b) { return a > b ? a : b; }
+  static __device__ __forceinline__ u64 warp(u64 v) {
+    const unsigned hi = __reduce_max_sync(0xffffffffu, static_cast<unsigned>(v >> 32));
+    const unsigned lo = __reduce_max_sync(0xffffffffu, static_cast<unsigned>(v >> 32) == hi ? static_cast<unsigned>(v) : 0u);
+    return static_cast<u64>(hi) << 32 | lo;
+  }
+  static constexpr u64 none = 0;
+};
+struct Min {
+  using OfBlocks = Min;
+  static __device__ __forceinline__ u64 two(u64 a, u64 b) { return a < b ? a : b; }
+  static __device__ __forceinline__ u64 warp(u64 v) { return ~Max::warp(~v); }
+  static constexpr u64 none = ~0ull;
+};
+struct Nothing {  // a word that is not used
+  using OfBlocks = Nothing;
+  static __device__ __forceinline__ u64 two(u64, u64) { return 0; }
+  static __device__ __forceinline__ u64 warp(u64) { return 0; }
+  static constexpr u64 none = 0;
+};
+struct OfFirst {  // the sum of the blocks' first threads' words
+  using OfBlocks = Add;
+  static __device__ __forceinline__ u64 two(u64 a, u64 b) { return a + b; }
+  static __device__ __forceinline__ u64 warp(u64 v) { return v; }
+  static constexpr u64 none = 0;
+};
+__device__ __forceinline__ u64 bits_of(double v) { return static_cast<u64>(__double_as_longlong(v)); }
+__device__ __forceinline__ double double_of(u64 v) { return __longlong_as_double(static_cast<long long>(v)); }
+
+// Three words from every block of the row.  Used in turns: a block may write the next exchange while another still reads this one, not the one after
 // (the barrier of the next one is between them).
 struct Exchange {
-  u64 a[2][kSliceParts], b[2][kSliceParts];
-  u64 warp_a[kSliceWarps], warp_b[kSliceWarps];
+  u64 a[2][kSliceParts], b[2][kSliceParts], c[2][kSliceParts];
+  u64 warp_a[kSliceWarps], warp_b[kSliceWarps], warp_c[kSliceWarps];
 };
-
 struct Words {
-  u64 a, b;
+  u64 a, b, c;
 };
-// Both words reduced over the row (fa, fb: of two words), the same in every thread.  `turn` counts the exchanges of the kernel.  Every block has
-// started (the caller has waited once for the cluster) and all threads come here.
-template <class FA, class FB>
-__device__ __forceinline__ Words exchange(Exchange& x, int& turn, int parts, int rank, u64 a, u64 b, FA&& fa, FB&& fb) {
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) {
-    a = fa(a, __shfl_xor_sync(0xffffffffu, a, d));
-    b = fb(b, __shfl_xor_sync(0xffffffffu, b, d));
-  }
+// The words reduced over the row, the same in every thread.  `turn` counts the exchanges of the kernel.  Every block has started (the caller has waited once for
+// the cluster) and all threads come here.
+template <class A, class B = Nothing, class C = Nothing>
+__device__ __forceinline__ Words exchange(Exchange& x, int& turn, int parts, int rank, u64 a, u64 b = 0, u64 c = 0) {
+  constexpr bool kB = !std::is_same<B, Nothing>::value, kC = !std::is_same<C, Nothing>::value;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = turn & 1;
   ++turn;
+  a = A::warp(a);
+  if (kB) b = B::warp(b);
+  if (kC) c = C::warp(c);
   if (lane == 0) {
     x.warp_a[warp] = a;
-    x.warp_b[warp] = b;
+    if (kB) x.warp_b[warp] = b;
+    if (kC) x.warp_c[warp] = c;
   }
   __syncthreads();
   if (warp == 0) {
-    a = x.warp_a[lane & (kSliceWarps - 1)];
-    b = x.warp_b[lane & (kSliceWarps - 1)];
-#pragma unroll
-    for (int d = kSliceWarps / 2; d > 0; d >>= 1) {
-      a = fa(a, __shfl_xor_sync(0xffffffffu, a, d));
-      b = fb(b, __shfl_xor_sync(0xffffffffu, b, d));
-    }
+    const auto block = [&](auto word, const u64 (&of)[kSliceWarps]) {
+      using W = decltype(word);
+      if (std::is_same<W, OfFirst>::value) return of[0];
+      return W::warp(lane < kSliceWarps ? of[lane & (kSliceWarps - 1)] : W::none);
+    };
+    a = block(A(), x.warp_a);
+    if (kB) b = block(B(), x.warp_b);
+    if (kC) c = block(C(), x.warp_c);
     if (parts == 1) {
       if (lane == 0) {
         x.a[t][0] = a;
-        x.b[t][0] = b;
+        if (kB) x.b[t][0] = b;
+        if (kC) x.c[t][0] = c;
       }
     } else if (lane < parts) {
-      *of_rank(&x.a[t][rank], lane) = a;
-      *of_rank(&x.b[t][rank], lane) = b;
+      Exchange* o = of_rank(&x, lane);
+      o->a[t][rank] = a;
+      if (kB) o->b[t][rank] = b;
+      if (kC) o->c[t][rank] = c;
     }
   }
   row_barrier(parts);
-  Words w = {x.a[t][0], x.b[t][0]};
-  for (int r = 1; r < parts; ++r) {
-    w.a = fa(w.a, x.a[t][r]);
-    w.b = fb(w.b, x.b[t][r]);
-  }
+  const auto row = [&](auto word, const u64 (&of)[kSliceParts]) {  // (by every warp: a loop over the blocks takes longer)
+    using W = typename decltype(word)::OfBlocks;
+    return W::warp(lane < parts ? of[lane & (kSliceParts - 1)] : W::none);
+  };
+  Words w = {row(A(), x.a[t]), 0, 0};
+  if (kB) w.b = row(B(), x.b[t]);
+  if (kC) w.c = row(C(), x.c[t]);
   return w;
 }
 
-// How many of `rows` rows' blocks: the fewest that fill the device twice over, within what a slice's shared memory and its least size allow.
+// How a row is cut up: as few blocks as `most` bytes of shared memory each allow (16 at most: what does not fit is read again where it is wanted), or more where
+// that leaves multiprocessors without two blocks, down to a vector a thread.  cluster: the blocks are one (a power of two).
 struct SlicePlan {
-  int parts, share, seg, res;
+  int parts, share, seg, res, sms;
   size_t smem;
 };
-cudaError_t slice_plan(int device, int rows, int vocab, int dtype, SlicePlan* plan);
+cudaError_t slice_plan(int device, int rows, int vocab, int dtype, int most, bool cluster, SlicePlan* plan);
 
 // Errors of the calls without a context (the text of cos_verify_last_error(NULL)).
 cos_status call_failed(cos_status st, const char* what);
@@ -201,21 +290,23 @@ struct OnDevice {
 };
 
 template <class P>
-cudaError_t slice_launch(void (*fn)(P), const P& p, int blocks, int parts, size_t smem, cudaStream_t stream) {
+cudaError_t slice_launch(void (*fn)(P), const P& p, int blocks, int parts, size_t smem, cudaStream_t stream, int threads = kSliceThreads) {
   cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e == cudaSuccess && parts > 8) e = cudaFuncSetAttribute(fn, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3(static_cast<unsigned>(blocks), 1, 1);
-  lc.blockDim = dim3(kSliceThreads, 1, 1);
+  lc.blockDim = dim3(static_cast<unsigned>(threads), 1, 1);
   lc.dynamicSmemBytes = smem;
   lc.stream = stream;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = static_cast<unsigned>(parts);
-  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = static_cast<unsigned>(parts);
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
   lc.attrs = at;
-  lc.numAttrs = parts > 1 ? 1 : 0;
+  lc.numAttrs = parts > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&lc, fn, p);
 }
 

@@ -11,6 +11,7 @@ from typing import Optional, Sequence
 from .binding import COS_MAX_MODELS, COS_OK, CosVerifyError, _current_stream, _dtype_code, load_library
 
 COS_TOP_MAX = 1024
+COS_DISTILL_STATISTICS = 8
 
 EXPORTS = ("cos_sample", "cos_top_logits", "cos_distill_loss", "cos_distill_grad", "cos_distill_step")
 
@@ -179,7 +180,7 @@ def _loss_call(student, ids, values, lse, weights, temperature, stream=None):
     import torch
     a = _distill_args(torch, student, ids, values, lse, weights, temperature)
     loss = torch.empty((a.rows,), dtype=torch.float32, device=student.device)
-    statistics = torch.empty((a.rows, 2), dtype=torch.float32, device=student.device)
+    statistics = torch.empty((a.rows * (COS_DISTILL_STATISTICS + a.lists * a.k),), dtype=torch.float32, device=student.device)
     a.loss, a.statistics = loss.data_ptr(), statistics.data_ptr()
     lib = _library()
     _check(lib, lib.cos_distill_loss(ctypes.byref(a), _stream_of(torch, student.device, stream, (loss, statistics))))
@@ -239,7 +240,7 @@ def distill_loss(student, ids, values, lse=None, weights: Optional[Sequence[floa
 def distill_step(student, ids, values, row_weights, lse=None, weights: Optional[Sequence[float]] = None, temperature: float = 1.0,
                  grad=None, stream=None) -> dict:
     """cos_distill_step: "loss" [rows] as of `distill_loss`, and "grad" [rows, vocab], the gradient of sum_n row_weights[n] loss[n] in
-    the student's logits, in one launch that reads them once; for training loops that know the weights of the rows beforehand
+    the student's logits, reading them once; for training loops that know the weights of the rows beforehand
     (1 / rows for a mean).  `grad`: a tensor that takes the gradient (`student` itself: in place)."""
     import torch
     a = _distill_args(torch, student, ids, values, lse, weights, temperature)
@@ -253,7 +254,9 @@ def distill_step(student, ids, values, row_weights, lse=None, weights: Optional[
     rows, vocab, a.stride_grad = _rows(grad, "grad")
     if (rows, vocab) != (a.rows, a.vocab) or grad.dtype != student.dtype or grad.device != device:
         raise ValueError("grad must be like the student's logits")
-    a.loss, a.grad = loss.data_ptr(), grad.data_ptr()
+    statistics = torch.empty((a.rows * (COS_DISTILL_STATISTICS + a.lists * a.k),), dtype=torch.float32, device=device)
+    made.append(statistics)
+    a.loss, a.statistics, a.grad = loss.data_ptr(), statistics.data_ptr(), grad.data_ptr()
     lib = _library()
     _check(lib, lib.cos_distill_step(ctypes.byref(a), _stream_of(torch, device, stream, made)))
     return {"loss": loss, "grad": grad}

@@ -49,7 +49,7 @@ def call_path() -> str:
 
 
 def call_needs_build() -> bool:
-    return _stale(call_path(), [CALL_SOURCE, os.path.join(INCLUDE, "cos_verify.h")])
+    return _stale(call_path(), [CALL_SOURCE] + sorted(glob.glob(os.path.join(INCLUDE, "*.h"))))
 
 
 def _compile(src: str, verbose: bool):

@@ -8,7 +8,7 @@ from __future__ import annotations
 import ctypes
 from typing import Optional, Sequence
 
-from .binding import COS_MAX_MODELS, COS_OK, CosVerifyError, _current_stream, _dtype_code, load_library
+from .binding import COS_MAX_MODELS, COS_OK, CosVerifyError, _current_stream, _dtype_code, load_call, load_library
 
 COS_TOP_MAX = 1024
 COS_DISTILL_STATISTICS = 8
@@ -46,6 +46,7 @@ class cos_distill_args(ctypes.Structure):
 
 
 _lib = None
+_native = None      # the module of csrc/call.cpp and the addresses of the functions it calls, or False
 
 
 def _library() -> ctypes.CDLL:
@@ -58,6 +59,15 @@ def _library() -> ctypes.CDLL:
             fn.restype = ctypes.c_int
         _lib = lib
     return _lib
+
+
+def _calls():
+    """The calls in native code, (module, address of each of EXPORTS): what plain tensors go through.  False where there is none."""
+    global _native
+    if _native is None:
+        lib, call = _library(), load_call()
+        _native = (call, *(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in EXPORTS)) if call is not None else False
+    return _native
 
 
 def _check(lib, st: int):
@@ -104,6 +114,14 @@ def sample(logits, uniforms, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, fil
     [rows]), "prob" (float32 [rows], under the law the token was drawn from) and, where `filtered` is true or a tensor that
     takes them (`logits` itself: in place), "filtered": the logits with -inf at the tokens that were not kept.  As the
     proposer's logits of a verification at the same temperature these are the law its drafts were drawn from."""
+    native = _calls() if stream is None else None
+    if native:
+        got = native[0].sample(native[1], logits, uniforms, temperature, top_k, top_p, min_p, filtered)
+        if type(got) is dict:
+            return got
+        if got is not None:
+            _check(_lib, got)
+    # (what does not fit there, and whatever there is to complain about)
     import torch
     rows, vocab, stride = _rows(logits, "logits")
     device = logits.device
@@ -137,6 +155,13 @@ def sample(logits, uniforms, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, fil
 def top_logits(logits, k: int, temperature: float = 1.0, stream=None) -> dict:
     """cos_top_logits: "values" (float32) and "ids" (int32), [rows, k], of the k largest logits of each row, the largest first,
     and "lse" [rows] float32, ln sum_x exp(l(x) / temperature): what `distill_loss` takes of a teacher."""
+    native = _calls() if stream is None else None
+    if native:
+        got = native[0].top_logits(native[2], logits, k, temperature)
+        if type(got) is dict:
+            return got
+        if got is not None:
+            _check(_lib, got)
     import torch
     rows, vocab, stride = _rows(logits, "logits")
     device = logits.device
@@ -228,6 +253,13 @@ def distill_loss(student, ids, values, lse=None, weights: Optional[Sequence[floa
     teachers' at the same temperature) shares are probabilities and what is not listed is left out; without, each list is
     taken to be the teacher's whole distribution.  `weights` are the ensemble's.  Differentiable in the student's logits alone, once.
     A row without entries has loss 0 and gradient 0, and a row whose upstream gradient is 0 has gradient 0, whatever its logits."""
+    native = _calls()
+    if native:
+        got = native[0].distill_loss(native[3], native[4], student, ids, values, lse, weights, temperature)
+        if type(got) is int:
+            _check(_lib, got)
+        elif got is not None:
+            return got
     import torch
     if torch.is_grad_enabled() and student.requires_grad:
         global _distill_function
@@ -242,6 +274,13 @@ def distill_step(student, ids, values, row_weights, lse=None, weights: Optional[
     """cos_distill_step: "loss" [rows] as of `distill_loss`, and "grad" [rows, vocab], the gradient of sum_n row_weights[n] loss[n] in
     the student's logits, reading them once; for training loops that know the weights of the rows beforehand
     (1 / rows for a mean).  `grad`: a tensor that takes the gradient (`student` itself: in place)."""
+    native = _calls() if stream is None and grad is None else None
+    if native:
+        got = native[0].distill_step(native[5], student, ids, values, lse, weights, temperature, row_weights)
+        if type(got) is dict:
+            return got
+        if got is not None:
+            _check(_lib, got)
     import torch
     a = _distill_args(torch, student, ids, values, lse, weights, temperature)
     device = student.device

@@ -9,10 +9,6 @@
 // launch with both stay in the shared memory of a cluster of blocks between the normaliser and the gradient, and are read once.  Three blocks of a multiprocessor
 // have up to 64 KB each under way, since a row's chain of steps (copies, two sweeps, a barrier, the gradient) takes longer than its bytes.
 // Exponentials are 32-bit (2^-22) and sums of them 64-bit; shares, logarithms and the loss are 64-bit; the gradient is rounded once.
-#include <cuda_bf16.h>
-
-#include <type_traits>
-
 #include "cos_slice.cuh"
 
 namespace cosv {
@@ -125,47 +121,27 @@ __device__ __forceinline__ void store_entry(char* row, int x, float v) {
     reinterpret_cast<__half*>(row)[x] = __float2half_rn(v);
 }
 
-template <int DT>
-__device__ __forceinline__ uint4 packed(const float (&v)[Elem<DT>::E]) {
-  uint4 r;
-  unsigned* w = reinterpret_cast<unsigned*>(&r);
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    if constexpr (DT == COS_DTYPE_F32) {
-      w[k] = __float_as_uint(v[k]);
-    } else if constexpr (DT == COS_DTYPE_BF16) {
-      const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
-      w[k] = *reinterpret_cast<const unsigned*>(&h);
-    } else {
-      const __half2 h = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
-      w[k] = *reinterpret_cast<const unsigned*>(&h);
-    }
-  }
-  return r;
-}
-
-// A vector of the gradient.
-template <int DT>
-__device__ __forceinline__ void write_vector(const RowSlice<DT>& s, char* row, int i, const float (&v)[Elem<DT>::E]) {
-  constexpr int E = Elem<DT>::E, B = Elem<DT>::bytes;
-  const int x = s.token(i);
-  if (static_cast<int>(reinterpret_cast<unsigned long long>(row) & 15) / B == s.off && x >= 0 && x <= s.V - E) {
-    *reinterpret_cast<uint4*>(row + static_cast<long long>(x) * B) = packed<DT>(v);
-  } else {
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-      if (x + e >= 0 && x + e < s.V) store_entry<DT>(row, x + e, v[e]);
-  }
-}
-// The slice of the gradient: f(values) in place of the values.
+// The slice of the gradient: f(vector) in place of the vectors (read: they are looked at).
 template <int DT, class F>
 __device__ __forceinline__ void write_slice(const RowSlice<DT>& s, char* row, bool read, F&& f) {
-  constexpr int E = Elem<DT>::E;
+  constexpr int E = Elem<DT>::E, B = Elem<DT>::bytes;
+  const bool whole = static_cast<int>(reinterpret_cast<unsigned long long>(row) & 15) / B == s.off;
   for (int i = s.begin + (threadIdx.x & 31); i < s.end; i += 32) {
-    float v[E] = {};
-    if (read) Elem<DT>::unpack(s.at(i), v);
-    f(v);
-    write_vector<DT>(s, row, i, v);
+    const uint4 g = f(read ? s.at(i) : uint4());
+    const int x = s.token(i);
+    if (whole && x >= 0 && x <= s.V - E) {
+      *reinterpret_cast<uint4*>(row + static_cast<long long>(x) * B) = g;
+    } else {
+      const unsigned* w = reinterpret_cast<const unsigned*>(&g);
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (x + e >= 0 && x + e < s.V) {
+          if (DT == COS_DTYPE_F32)
+            reinterpret_cast<unsigned*>(row)[x + e] = w[e];
+          else
+            reinterpret_cast<unsigned short*>(row)[x + e] = static_cast<unsigned short>((e & 1) ? w[e >> 1] >> 16 : w[e >> 1]);
+        }
+    }
   }
 }
 
@@ -177,25 +153,9 @@ struct Normaliser {
 struct NormaliserRoom {
   Normaliser warp[kSliceWarps], block[kSliceParts];
 };
-template <int DT>
-__device__ __forceinline__ Normaliser normaliser(NormaliserRoom& room, const RowSlice<DT>& s, int parts, int rank, float c) {
-  constexpr int E = Elem<DT>::E;
+// ... from the warps' (m the same for the lanes of one, z a lane's).
+__device__ __forceinline__ Normaliser row_normaliser(NormaliserRoom& room, int parts, int rank, float c, float m, double z) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  float m = -INFINITY;
-  s.vectors([&](int, const float (&v)[E]) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) m = max_nan(m, v[e]);
-  });
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, d));
-  double z = 0.0;
-  if (!(m == -INFINITY))  // (NaN: all NaN)
-    s.vectors([&](int, const float (&v)[E]) {
-      float part = 0.0f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) part += ex2_approx((v[e] - m) * c);
-      z += static_cast<double>(part);
-    });
   z = warp_sum(z);
   if (lane == 0) room.warp[warp] = {m, z};
   __syncthreads();
@@ -223,11 +183,44 @@ __device__ __forceinline__ Normaliser normaliser(NormaliserRoom& room, const Row
   return n;
 }
 
-// q(x) times the scale, from the statistics of the student.
-template <int E>
-__device__ __forceinline__ void to_gradient(float (&v)[E], float scale, float m, float c, float log_z) {
+template <int DT>
+__device__ __forceinline__ Normaliser normaliser(NormaliserRoom& room, const RowSlice<DT>& s, int parts, int rank, float c) {
+  RunningMax<DT> top;
+  s.raw([&](int, const uint4& r) { top.add(r); });
+  float m = top.value();
 #pragma unroll
-  for (int e = 0; e < E; ++e) v[e] = scale * ex2_approx((v[e] - m) * c - log_z);
+  for (int d = 16; d > 0; d >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, d));
+  double z = 0.0;
+  if (!(m == -INFINITY)) {  // (NaN: all NaN)
+    const f32x2 minus_m = pack2(-m, -m), cc = pack2(c, c);
+    s.raw([&](int, const uint4& r) { z += static_cast<double>(sum_exp2<DT>(r, minus_m, cc)); });
+  }
+  return row_normaliser(room, parts, rank, c, m, z);
+}
+
+// q(x) times the scale, from the statistics of the student.
+template <int DT>
+__device__ __forceinline__ uint4 gradient_of(const uint4& r, f32x2 scale, f32x2 minus_m, f32x2 c, f32x2 minus_log_z) {
+  f32x2 x[Elem<DT>::E / 2];
+  unpack_pairs<DT>(r, x);
+  uint4 g;
+  unsigned* w = reinterpret_cast<unsigned*>(&g);
+#pragma unroll
+  for (int k = 0; k < Elem<DT>::E / 2; ++k) {
+    const f32x2 a = fma2(add2(x[k], minus_m), c, minus_log_z);
+    const f32x2 e = mul2(pack2(ex2_approx(lo2(a)), ex2_approx(hi2(a))), scale);
+    if constexpr (DT == COS_DTYPE_F32) {
+      w[2 * k] = __float_as_uint(lo2(e));
+      w[2 * k + 1] = __float_as_uint(hi2(e));
+    } else if constexpr (DT == COS_DTYPE_BF16) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(lo2(e), hi2(e));
+      w[k] = *reinterpret_cast<const unsigned*>(&h);
+    } else {
+      const __half2 h = __floats2half2_rn(lo2(e), hi2(e));
+      w[k] = *reinterpret_cast<const unsigned*>(&h);
+    }
+  }
+  return g;
 }
 // The gradient at a listed token.
 __device__ __forceinline__ float listed_gradient(float s, double t, double per, double mass, float m, float c, float log_z) {
@@ -280,12 +273,57 @@ __global__ void __launch_bounds__(kShareThreads) cos_distill_shares_kernel(const
   if (threadIdx.x == 0) *statistics_of(p, row) = {0.0f, 0.0f, static_cast<float>(mass), static_cast<float>(base), listed, mass};
 }
 
+__device__ __forceinline__ float log2_of(const Normaliser& z) { return z.m == -INFINITY ? __int_as_float(0x7fc00000) : static_cast<float>(log2(z.z)); }
+__device__ __forceinline__ void finish_loss(const DistillParams& p, int row, const Statistics& st, const Normaliser& z, bool keep) {
+  const double inv_T = 1.0 / static_cast<double>(p.T);
+  const float log_z = log2_of(z);
+  p.loss[row] = z.m == -INFINITY ? log_z : static_cast<float>(st.listed + st.mass64 * ((static_cast<double>(z.m) - static_cast<double>(st.reference)) * inv_T + log(z.z)));
+  if (keep) {
+    statistics_of(p, row)->m = z.m;
+    statistics_of(p, row)->log_z = log_z;
+  }
+}
+
+// The loss where there are rows enough for a block each: a row goes by in registers, against a running maximum of each lane.
+template <int DT>
+__global__ void __launch_bounds__(kSliceThreads, 3) cos_distill_stream_kernel(const DistillParams p) {
+  __shared__ NormaliserRoom room;
+  const int row = blockIdx.x;
+  RowSlice<DT> s;
+  s.init(p.student + static_cast<long long>(row) * p.stride * Elem<DT>::bytes, p.V, 0, p.share, p.seg, nullptr, 0);
+  wait_for_inputs();
+  const Statistics st = *statistics_of(p, row);
+  if (st.mass64 == 0.0) {
+    if (threadIdx.x == 0) p.loss[row] = 0.0f;
+    return;
+  }
+  const float c = fminf(static_cast<float>(1.4426950408889634 / static_cast<double>(p.T)), 3e38f);
+  const f32x2 cc = pack2(c, c);
+  float m = -INFINITY;
+  double z = 0.0;
+  s.stream(s.begin + (threadIdx.x & 31), s.end, [&](const uint4& r) {
+    RunningMax<DT> top;
+    top.add(r);
+    const float t = top.value();
+    if (t > m || t != t) {  // (a maximum that is NaN stays it)
+      z *= static_cast<double>(m == -INFINITY ? 0.0f : ex2_approx((m - t) * c));
+      m = t;
+    }
+    if (m != -INFINITY) z += static_cast<double>(sum_exp2<DT>(r, pack2(-m, -m), cc));
+  });
+  float all = m;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) all = max_nan(all, __shfl_xor_sync(0xffffffffu, all, d));
+  if (m != -INFINITY) z *= static_cast<double>(ex2_approx((m - all) * c));
+  const Normaliser n = row_normaliser(room, 1, 0, c, all, z);
+  if (threadIdx.x == 0) finish_loss(p, row, st, n, true);
+}
+
 // The rows.  kGrad: the normalisers are there, and every block works for itself.
 template <int DT, int MODE>
 __global__ void __launch_bounds__(kSliceThreads, 3) cos_distill_kernel(const DistillParams p) {
   extern __shared__ uint4 smem[];
   __shared__ NormaliserRoom room;
-  constexpr int E = Elem<DT>::E;
   const int parts = p.parts, rank = blockIdx.x % parts, row = blockIdx.x / parts, tid = threadIdx.x, n = p.lists * p.k;
   const bool wide = MODE != kGrad && parts > 1;
   if (wide) cluster_barrier_arrive();
@@ -301,7 +339,7 @@ __global__ void __launch_bounds__(kSliceThreads, 3) cos_distill_kernel(const Dis
   const bool none = st.mass64 == 0.0;
   if (none || (MODE == kGrad && weight == 0.0f)) {
     if (MODE != kGrad && rank == 0 && tid == 0) p.loss[row] = 0.0f;
-    if (MODE != kLoss) write_slice<DT>(s, grad, false, [](float (&)[E]) {});
+    if (MODE != kLoss) write_slice<DT>(s, grad, false, [](const uint4& nothing) { return nothing; });
     s.finish();
     if (wide) cluster_barrier_wait();
     return;
@@ -331,28 +369,21 @@ __global__ void __launch_bounds__(kSliceThreads, 3) cos_distill_kernel(const Dis
   if (MODE != kGrad) {
     if (wide) cluster_barrier_wait();  // (every block of the row has started)
     const Normaliser z = normaliser<DT>(room, s, parts, rank, c);
-    const bool empty = z.m == -INFINITY;
     m = z.m;
-    log_z = empty ? __int_as_float(0x7fc00000) : static_cast<float>(log2(z.z));
-    if (rank == 0 && tid == 0) {
-      const double inv_T = 1.0 / static_cast<double>(p.T);
-      p.loss[row] = empty ? log_z : static_cast<float>(st.listed + st.mass64 * ((static_cast<double>(m) - static_cast<double>(st.reference)) * inv_T + log(z.z)));
-      if (MODE == kLoss) {
-        statistics_of(p, row)->m = m;
-        statistics_of(p, row)->log_z = log_z;
-      }
-    }
+    log_z = log2_of(z);
+    if (rank == 0 && tid == 0) finish_loss(p, row, st, z, MODE == kLoss);
   } else {
     __syncthreads();  // (the listed tokens have been read)
   }
   if (MODE != kLoss) {
     if (MODE == kStep && weight == 0.0f) {
-      write_slice<DT>(s, grad, false, [](float (&)[E]) {});
+      write_slice<DT>(s, grad, false, [](const uint4& nothing) { return nothing; });
       return;
     }
     const double per = static_cast<double>(weight) / static_cast<double>(p.T), mass = static_cast<double>(st.mass);
     const float scale = static_cast<float>(per * mass);
-    write_slice<DT>(s, grad, true, [&](float (&v)[E]) { to_gradient(v, scale, m, c, log_z); });
+    const f32x2 scales = pack2(scale, scale), minus_m = pack2(-m, -m), cc = pack2(c, c), minus_log_z = pack2(-log_z, -log_z);
+    write_slice<DT>(s, grad, true, [&](const uint4& r) { return gradient_of<DT>(r, scales, minus_m, cc, minus_log_z); });
     __syncthreads();  // (the listed tokens' places are written again)
 #pragma unroll
     for (int k = 0; k < 2; ++k)
@@ -404,6 +435,7 @@ cos_status distill(const cos_distill_args* a, void* cuda_stream) {
   p.seg = plan.seg;
   p.res = plan.res;
   p.early = 2 * plan.sms;
+  if (MODE == kLoss && a->rows >= 2 * plan.sms) plan_row(a->vocab, a->dtype, &p.share, &p.seg);
   p.lists = a->lists;
   p.k = a->k;
   p.ids = a->ids;
@@ -423,6 +455,7 @@ cos_status distill(const cos_distill_args* a, void* cuda_stream) {
       const cudaError_t first = slice_launch(cos_distill_shares_kernel<DT>, p, a->rows, 1, static_cast<size_t>(a->lists) * a->k * (sizeof(double) + sizeof(int)), stream, kShareThreads);
       if (first != cudaSuccess) return first;
     }
+    if (MODE == kLoss && a->rows >= 2 * plan.sms) return slice_launch(cos_distill_stream_kernel<DT>, p, a->rows, 1, 0, stream);
     return slice_launch(cos_distill_kernel<DT, MODE>, p, a->rows * plan.parts, MODE == kGrad ? 1 : plan.parts, plan.smem, stream);
   };
   e = a->dtype == COS_DTYPE_F32    ? launches(std::integral_constant<int, COS_DTYPE_F32>())

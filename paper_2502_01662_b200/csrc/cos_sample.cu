@@ -300,6 +300,18 @@ __device__ __forceinline__ void list(H& h, float v, int token) {
   const int at = atomicAdd(&h.listed, 1);
   if (at < static_cast<int>(sizeof(h.list) / sizeof(u64))) h.list[at] = place_of(v, token);
 }
+// ... those of a vector from a logit on.
+template <int DT, class H>
+__device__ __forceinline__ void list_from(H& h, float from, int token, const uint4& r) {
+  RunningMax<DT> top;
+  top.add(r);
+  if (top.value() >= from)
+#pragma unroll 1
+    for (int e = 0; e < Elem<DT>::E; ++e) {
+      const float v = Weight<DT>::pick(r, e);
+      if (v >= from && v > -INFINITY) list(h, v, token + e);
+    }
+}
 // Behind the sweep that listed them (h.listed was 0): how many candidates the row has, and the sums over the row of `sum` and of the lanes' masses of what
 // they listed.
 struct Taken {
@@ -575,17 +587,30 @@ __device__ __forceinline__ void write_filtered(const RowSlice<DT>& s, char* row,
 struct Groups {
   float largest, smallest, own, group;
 };
+// largest and smallest from every thread's: `top` the largest of its groups, `low` the smallest above -inf (or -inf).
+template <class H>
+__device__ __forceinline__ void group_range(H& h, Groups& g, float top, float low) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const unsigned hi = __reduce_max_sync(0xffffffffu, top != top ? 0xffffffffu : ordered(top));  // (NaN above all)
+  const unsigned lo = __reduce_min_sync(0xffffffffu, low == -INFINITY ? 0xffffffffu : ordered(low));
+  if (lane == 0) {
+    h.scan_count[warp] = hi;
+    h.scan_mass[warp] = lo;
+  }
+  __syncthreads();
+  const unsigned all = __reduce_max_sync(0xffffffffu, static_cast<unsigned>(h.scan_count[lane & (kSliceWarps - 1)]));
+  const unsigned least = __reduce_min_sync(0xffffffffu, static_cast<unsigned>(h.scan_mass[lane & (kSliceWarps - 1)]));
+  g.largest = all == 0xffffffffu ? __int_as_float(0x7fc00000) : unordered(all);
+  g.smallest = least == 0xffffffffu ? g.largest : unordered(least);
+}  // (the two arrays are written next behind a barrier of the block)
 template <int DT, class H>
 __device__ __forceinline__ Groups group_max(Row<H>& w, const RowSlice<DT>& s) {
-  constexpr int E = Elem<DT>::E;
   const int tid = threadIdx.x, lane = tid & 31;
   Groups g;
   s.finish();
-  float m = -INFINITY;
-  s.vectors([&](int, const float (&v)[E]) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) m = max_nan(m, v[e]);
-  });
+  RunningMax<DT> here;
+  s.raw([&](int, const uint4& r) { here.add(r); });
+  float m = here.value();
   g.own = m;
   for (int d = 1; d < w.parts; d <<= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, d));
   if (w.parts > 1) {
@@ -597,27 +622,19 @@ __device__ __forceinline__ Groups group_max(Row<H>& w, const RowSlice<DT>& s) {
   }
   row_barrier(w.parts);
   g.group = w.h.group[tid];
-  const unsigned key = g.group != g.group ? 0xffffffffu : ordered(g.group);  // (NaN above all)
-  const unsigned hi = __reduce_max_sync(0xffffffffu, key), lo = __reduce_min_sync(0xffffffffu, g.group == -INFINITY ? 0xffffffffu : key);
-  if (lane == 0) {
-    w.h.scan_count[tid >> 5] = hi;
-    w.h.scan_mass[tid >> 5] = lo;
-  }
-  __syncthreads();
-  const unsigned top = __reduce_max_sync(0xffffffffu, static_cast<unsigned>(w.h.scan_count[lane & (kSliceWarps - 1)]));
-  const unsigned low = __reduce_min_sync(0xffffffffu, static_cast<unsigned>(w.h.scan_mass[lane & (kSliceWarps - 1)]));
-  g.largest = top == 0xffffffffu ? __int_as_float(0x7fc00000) : unordered(top);
-  g.smallest = low == 0xffffffffu ? g.largest : unordered(low);
-  return g;  // (the two arrays are written next behind a barrier of the block)
+  group_range(w.h, g, g.group, g.group);
+  return g;
 }
 
 // A logit that at least k of the groups reach, the largest one up to 1/64 of the range that the groups' largest logits span; -inf where fewer groups have a token.
-// h.steps is 0, and is again.
-template <class H>
-__device__ __forceinline__ float reached_by(H& h, const Groups& g, int k) {
+// own: this thread's groups.  h.steps is 0, and is again.
+template <class H, int N>
+__device__ __forceinline__ float reached_by(H& h, const Groups& g, const float (&own)[N], int k) {
   const int tid = threadIdx.x, lane = tid & 31;
   const float span = g.largest - g.smallest, per = 64.0f / span;  // (span: overflows to inf for logits further apart than floats go: all in the first step)
-  if (g.group > -INFINITY) atomicAdd(&h.steps[min(static_cast<int>((g.largest - g.group) * per), 63)], 1u);
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (own[i] > -INFINITY) atomicAdd(&h.steps[min(static_cast<int>((g.largest - own[i]) * per), 63)], 1u);
   __syncthreads();
   const unsigned a = h.steps[2 * lane], b = h.steps[2 * lane + 1];
   unsigned up = a + b;
@@ -723,7 +740,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
     u64 total = 0;  // what top-p is a part of
     bool counted = false;
     if (!by_k || k <= kHeadMost) {
-      const float from = reached_by(h, groups, by_k ? k : min(kHeadGuess, p.c.V));
+      const float from = reached_by(h, groups, {groups.group}, by_k ? k : min(kHeadGuess, p.c.V));
       u64 sum = 0, mass = 0;
       if (!by_k) {  // (everything is looked at for the total; the histogram is filled on the way, for rows that want it)
         s.raw([&](int token, const uint4& r) {
@@ -740,9 +757,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
         });
         counted = true;
       } else if (own >= from) {
-        s.entries([&](int token, float v) {
-          if (v >= from && v > -INFINITY) list(h, v, token);
-        });
+        s.raw([&](int token, const uint4& r) { list_from<DT>(h, from, token, r); });
       }
       const Taken got = taken<Add, Add>(w, sum, mass);
       total = got.sum;
@@ -879,22 +894,52 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
   if (filtered) write_filtered<DT>(s, filtered, keeps);
 }
 
-template <int DT, int kList>
-__global__ void __launch_bounds__(kSliceThreads, 3) cos_top_kernel(const TopParams p) {
+// kStream: a block for each row, which goes by in registers; what has candidates in it is read again.
+template <int DT, int kList, bool kStream>
+__global__ void __launch_bounds__(kSliceThreads, kStream ? 3 : 2) cos_top_kernel(const TopParams p) {
   extern __shared__ uint4 smem[];
   Shared<kList>& h = *reinterpret_cast<Shared<kList>*>(smem);
   __shared__ Exchange x;
-  const int parts = p.c.parts, rank = blockIdx.x % parts, row = blockIdx.x / parts, tid = threadIdx.x;
+  constexpr int kGroups = kStream ? 2 : 1;  // of a thread
+  const int parts = kStream ? 1 : p.c.parts, rank = kStream ? 0 : blockIdx.x % parts, row = kStream ? blockIdx.x : blockIdx.x / parts, tid = threadIdx.x;
   if (parts > 1) cluster_barrier_arrive();
   wait_for_inputs();
   RowSlice<DT> s;
   s.init(static_cast<const char*>(p.c.logits) + static_cast<long long>(row) * p.c.stride * Elem<DT>::bytes, p.c.V, rank, p.c.share, p.c.seg, smem + sizeof(h) / 16, p.c.res);
-  s.start();
   if (tid < 64) h.steps[tid] = 0;
   if (tid == 0) h.listed = 0;
   Row<Shared<kList>> w = {h, x, parts, rank, 0, 0};
-  const Groups groups = group_max(w, s);
-  const float m = groups.largest, own = groups.own;
+  const float c = fminf(static_cast<float>(1.4426950408889634 / static_cast<double>(p.T)), 3e38f);
+  const f32x2 cc = pack2(c, c);
+  const int half = (p.c.seg / 32 + kGroups - 1) / kGroups * 32;  // vectors of a warp's groups
+  Groups groups;
+  float own[kGroups], mine = -INFINITY;  // the largest of this thread's groups, and of them
+  double sum = 0.0;                      // against `mine`
+  if constexpr (kStream) {
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      RunningMax<DT> group;
+      s.stream(s.begin + (tid & 31) + g * half, min(s.end, s.begin + (g + 1) * half), [&](const uint4& r) {
+        RunningMax<DT> top;
+        top.add(r);
+        group.add(r);
+        const float t = top.value();
+        if (t > mine || t != t) {  // (a maximum that is NaN stays it)
+          sum *= static_cast<double>(mine == -INFINITY ? 0.0f : ex2_approx((mine - t) * c));
+          mine = t;
+        }
+        if (mine != -INFINITY) sum += static_cast<double>(sum_exp2<DT>(r, pack2(-mine, -mine), cc));
+      });
+      own[g] = group.value();
+    }
+    group_range(h, groups, mine, own[0] == -INFINITY ? own[1] : own[1] == -INFINITY ? own[0] : fminf(own[0], own[1]));
+  } else {
+    s.start();
+    groups = group_max(w, s);
+    own[0] = groups.group;
+    mine = groups.own;
+  }
+  const float m = groups.largest;
   float* const values = p.values + static_cast<long long>(row) * p.k;
   int* const ids = p.ids + static_cast<long long>(row) * p.k;
   if (!(m > -INFINITY && m < INFINITY)) {
@@ -907,21 +952,23 @@ __global__ void __launch_bounds__(kSliceThreads, 3) cos_top_kernel(const TopPara
     }
     return;
   }
-  const float c = fminf(static_cast<float>(1.4426950408889634 / static_cast<double>(p.T)), 3e38f);
-  double sum = 0.0;
-  s.vectors([&](int, const float (&v)[RowSlice<DT>::E]) {
-    float part = 0.0f;  // (of a vector: eight terms of at most 1)
-#pragma unroll
-    for (int e = 0; e < RowSlice<DT>::E; ++e) part += ex2_approx((v[e] - m) * c);
-    sum += static_cast<double>(part);
-  });
+  if constexpr (kStream) {
+    if (mine != -INFINITY) sum *= static_cast<double>(ex2_approx((mine - m) * c));
+  } else {
+    const f32x2 minus_m = pack2(-m, -m);
+    s.raw([&](int, const uint4& r) { sum += static_cast<double>(sum_exp2<DT>(r, minus_m, cc)); });
+  }
   int n = kList + 1;
   if (p.k <= kHeadMost) {
-    const float from = reached_by(h, groups, p.k);
-    if (own >= from)
-      s.entries([&](int token, float v) {
-        if (v >= from && v > -INFINITY) list(h, v, token);
-      });
+    const float from = reached_by(h, groups, own, p.k);
+    if constexpr (kStream) {
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g)
+        if (own[g] >= from)
+          for (int i = s.begin + (tid & 31) + g * half; i < min(s.end, s.begin + (g + 1) * half); i += 32) list_from<DT>(h, from, s.token(i), s.fetch(i));
+    } else if (mine >= from) {
+      s.raw([&](int token, const uint4& r) { list_from<DT>(h, from, token, r); });
+    }
     const Taken got = taken<AddDouble>(w, bits_of(sum));
     n = static_cast<int>(got.n);
     sum = double_of(got.sum);
@@ -1001,13 +1048,19 @@ cos_status check_rows(const void* logits, long long stride, int rows, int vocab,
 }
 
 template <class P, class F>
-cos_status launch_rows(P& p, int rows, int vocab, int dtype, int device, size_t shared, cudaStream_t stream, F&& kernel_of) {
+cos_status launch_rows(P& p, int rows, int vocab, int dtype, int device, size_t shared, bool whole, cudaStream_t stream, F&& kernel_of) {
   OnDevice on(device);
   if (on.error != cudaSuccess) return call_failed("cudaSetDevice", on.error);
   SlicePlan plan;
   cudaError_t e = slice_plan(device, rows, vocab, dtype, 44 * 1024, true, &plan);
   if (e != cudaSuccess) return call_failed("device query", e);
   if (static_cast<long long>(rows) * plan.parts > 0x7fffffffll) return call_failed(COS_ERR_UNSUPPORTED, "too many rows for one launch");
+  if (whole) {  // a block for each row, which stays in memory
+    plan.parts = 1;
+    plan.res = 0;
+    plan.smem = 0;
+    plan_row(vocab, dtype, &plan.share, &plan.seg);
+  }
   p.c.V = vocab;
   p.c.parts = plan.parts;
   p.c.share = plan.share;
@@ -1075,7 +1128,7 @@ extern "C" cos_status cos_sample(const cos_sample_args* a, void* cuda_stream) {
   p.status = a->row_status;
   p.filtered = static_cast<char*>(a->filtered);
   p.stride_filtered = a->stride_filtered;
-  return launch_rows(p, a->rows, a->vocab, a->dtype, a->device, sizeof(SampleShared), static_cast<cudaStream_t>(cuda_stream), [](int dt) {
+  return launch_rows(p, a->rows, a->vocab, a->dtype, a->device, sizeof(SampleShared), false, static_cast<cudaStream_t>(cuda_stream), [](int dt) {
     return dt == COS_DTYPE_F32 ? cos_sample_kernel<COS_DTYPE_F32> : (dt == COS_DTYPE_BF16 ? cos_sample_kernel<COS_DTYPE_BF16> : cos_sample_kernel<COS_DTYPE_F16>);
   });
 }
@@ -1096,11 +1149,17 @@ extern "C" cos_status cos_top_logits(const cos_top_args* a, void* cuda_stream) {
   p.values = a->values;
   p.ids = a->ids;
   p.lse = a->lse;
-  const auto call = [&](auto list) {
+  const auto call = [&](auto list, auto stream) {
     constexpr int kList = decltype(list)::value;
-    return launch_rows(p, a->rows, a->vocab, a->dtype, a->device, sizeof(Shared<kList>), static_cast<cudaStream_t>(cuda_stream), [](int dt) {
-      return dt == COS_DTYPE_F32 ? cos_top_kernel<COS_DTYPE_F32, kList> : (dt == COS_DTYPE_BF16 ? cos_top_kernel<COS_DTYPE_BF16, kList> : cos_top_kernel<COS_DTYPE_F16, kList>);
+    constexpr bool kStream = decltype(stream)::value;
+    return launch_rows(p, a->rows, a->vocab, a->dtype, a->device, sizeof(Shared<kList>), kStream, static_cast<cudaStream_t>(cuda_stream), [](int dt) {
+      return dt == COS_DTYPE_F32 ? cos_top_kernel<COS_DTYPE_F32, kList, kStream> : (dt == COS_DTYPE_BF16 ? cos_top_kernel<COS_DTYPE_BF16, kList, kStream> : cos_top_kernel<COS_DTYPE_F16, kList, kStream>);
     });
   };
-  return a->k <= kMost<kCandidates> ? call(std::integral_constant<int, kCandidates>()) : call(std::integral_constant<int, kTopCandidates>());
+  int sms = 0;
+  const cudaError_t e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, a->device);
+  if (e != cudaSuccess) return call_failed("device query", e);
+  using Few = std::integral_constant<int, kCandidates>;
+  if (a->k > kMost<kCandidates>) return call(std::integral_constant<int, kTopCandidates>(), std::false_type());
+  return a->rows >= 2 * sms ? call(Few(), std::true_type()) : call(Few(), std::false_type());
 }

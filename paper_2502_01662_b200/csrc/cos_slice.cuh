@@ -7,6 +7,8 @@
 #ifndef COS_SLICE_CUH
 #define COS_SLICE_CUH
 
+#include <cuda_bf16.h>
+
 #include <type_traits>
 
 #include "cos_common.cuh"
@@ -16,6 +18,56 @@ namespace cosv {
 
 constexpr int kSliceThreads = 512, kSliceWarps = kSliceThreads / 32, kSliceParts = 16;  // threads of a block, most blocks of a row
 typedef unsigned long long u64;
+
+__device__ __forceinline__ float max_nan(float a, float b) {  // NaN where one is
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+// The largest entry of vectors (NaN where there is one): 16-bit types two entries at a time.
+template <int DT>
+struct RunningMax {
+  unsigned top[DT == COS_DTYPE_F32 ? 2 : 1];
+  __device__ __forceinline__ RunningMax() {
+    for (unsigned& w : top) w = neg_inf_vector<DT>().x;
+  }
+  static __device__ __forceinline__ unsigned larger(unsigned a, unsigned b) {
+    if constexpr (DT == COS_DTYPE_F32) {
+      return __float_as_uint(max_nan(__uint_as_float(a), __uint_as_float(b)));
+    } else if constexpr (DT == COS_DTYPE_BF16) {
+      const __nv_bfloat162 m = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+      return *reinterpret_cast<const unsigned*>(&m);
+    } else {
+      const __half2 m = __hmax2_nan(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+      return *reinterpret_cast<const unsigned*>(&m);
+    }
+  }
+  __device__ __forceinline__ void add(const uint4& r) {
+    constexpr int kLast = DT == COS_DTYPE_F32 ? 1 : 0;
+    top[0] = larger(top[0], larger(r.x, r.z));
+    top[kLast] = larger(top[kLast], larger(r.y, r.w));
+  }
+  __device__ __forceinline__ float value() const {
+    if constexpr (DT == COS_DTYPE_F32) return max_nan(__uint_as_float(top[0]), __uint_as_float(top[1]));
+    const uint4 r = make_uint4(top[0], 0, 0, 0);
+    return max_nan(entry<DT>(r, 0), entry<DT>(r, 1));
+  }
+};
+
+// sum of 2^((v - m) c) over a vector's entries
+template <int DT>
+__device__ __forceinline__ float sum_exp2(const uint4& r, f32x2 minus_m, f32x2 c) {
+  f32x2 x[Elem<DT>::E / 2], sum = 0;
+  unpack_pairs<DT>(r, x);
+#pragma unroll
+  for (int k = 0; k < Elem<DT>::E / 2; ++k) {
+    const f32x2 a = mul2(add2(x[k], minus_m), c);
+    const f32x2 e = pack2(ex2_approx(lo2(a)), ex2_approx(hi2(a)));
+    sum = k == 0 ? e : add2(sum, e);
+  }
+  return lo2(sum) + hi2(sum);
+}
 
 template <int DT>
 struct RowSlice {
@@ -98,6 +150,23 @@ struct RowSlice {
       f(token(i), v);
     }
   }
+  // f(vector) for every vector of this lane in [from, to) of the slice, fetched from memory with several under way.
+  template <class F>
+  __device__ __forceinline__ void stream(int from, int to, F&& f) const {
+    constexpr int kAhead = 4;
+    uint4 r[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) r[k] = from + 32 * k < to ? fetch(from + 32 * k) : neg_inf_vector<DT>();
+    for (int i = from; i < to; i += 32 * kAhead) {
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const uint4 here = r[k];
+        const int next = i + 32 * (k + kAhead);
+        r[k] = next < to ? fetch(next) : neg_inf_vector<DT>();
+        f(here);
+      }
+    }
+  }
   // f(token of the first entry, vector) likewise.
   template <class F>
   __device__ __forceinline__ void raw(F&& f) const {
@@ -141,12 +210,6 @@ __device__ __forceinline__ void row_barrier(int parts) {
 template <class T>
 __device__ __forceinline__ T* of_rank(T* p, int rank) {
   return cg::this_cluster().map_shared_rank(p, rank);
-}
-
-__device__ __forceinline__ float max_nan(float a, float b) {  // NaN where one is
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
 }
 
 // How a word is reduced over a warp and over a few words.  (Reductions of 32 bits in one instruction where they do: a shuffle is one for each warp and clock of the
@@ -269,6 +332,12 @@ struct SlicePlan {
   int parts, share, seg, res, sms;
   size_t smem;
 };
+// (a whole row for one block)
+inline void plan_row(int vocab, int dtype, int* share, int* seg) {
+  const int E = dtype == COS_DTYPE_F32 ? 4 : 8;
+  *share = static_cast<int>((static_cast<long long>(vocab) + 2 * (E - 1)) / E);
+  *seg = (*share + 32 * kSliceWarps - 1) / (32 * kSliceWarps) * 32;
+}
 cudaError_t slice_plan(int device, int rows, int vocab, int dtype, int most, bool cluster, SlicePlan* plan);
 
 // Errors of the calls without a context (the text of cos_verify_last_error(NULL)).

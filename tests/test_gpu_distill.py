@@ -244,3 +244,21 @@ def test_streams_and_graphs():
                 graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(o["grad"], fresh["grad"]) and torch.equal(o["loss"], fresh["loss"]) for o in outs)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_many_rows(dtype):
+    """Rows enough for a block each."""
+    V, rows = 20001, 310
+    s, ids, values, lse = make(rows, V, dtype, 2, 24, seed=15, pad=1)
+    s[1, ::2] = -float("inf")
+    s[1, ids[1].flatten().long()] = 1.0
+    s[2] = torch.linspace(-20, 20, V, device="cuda").to(s.dtype)      # (a lane sees up to 6 new maxima: V / 8 / 512 + 1, or 11 of fp32)
+    s[3] = float("nan")
+    ids[3] = -1
+    check(s, ids, values, lse, [0.5, 0.5], 1.0)
+    s[4, 100] = float("nan")
+    s[5] = -float("inf")
+    s[6, 9] = float("inf")
+    loss = pkg.distill_loss(s, ids, values, lse, [0.5, 0.5])
+    assert loss[4:7].isnan().all() and loss[:4].isfinite().all() and loss[7:].isfinite().all()

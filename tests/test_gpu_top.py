@@ -110,3 +110,24 @@ def test_streams_and_graphs():
         graph.replay()
     fresh = check(x, 64, 1.0)
     assert all(torch.equal(out[n], fresh[n]) for n in out)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_many_rows(dtype):
+    """Rows enough for a block each: masks, ties and rows that are not finite among ordinary ones, unaligned rows."""
+    V, rows = 20001, 310
+    g = torch.Generator("cuda").manual_seed(5)
+    x = (2.5 * torch.randn((rows, V), generator=g, device="cuda")).to(DTYPES[dtype])
+    x[1] = 0.5
+    x[2] = -float("inf")
+    x[3, 10:] = -float("inf")
+    x[4, 5] = float("nan")
+    x[5, 7] = float("inf")
+    x[6] = torch.finfo(x.dtype).min
+    x[7, 1:] = torch.finfo(x.dtype).min
+    x[8] = torch.randint(0, 3, (V,), generator=g, device="cuda").to(x.dtype)
+    x[9] = torch.linspace(-1, 1, V, device="cuda").to(x.dtype) * 0.01
+    x[10] = torch.linspace(-20, 20, V, device="cuda").to(x.dtype)
+    x[11, ::2] = -float("inf")
+    for k in (1, 64, 288, 1000):
+        check(x, k, 1.0)

@@ -286,36 +286,42 @@ __device__ __forceinline__ void finish_loss(const DistillParams& p, int row, con
 
 // The loss where there are rows enough for a block each: a row goes by in registers, against a running maximum of each lane.
 template <int DT>
-__global__ void __launch_bounds__(kSliceThreads, 3) cos_distill_stream_kernel(const DistillParams p) {
+__global__ void __launch_bounds__(kSliceThreads, 2) cos_distill_stream_kernel(const DistillParams p) {
   __shared__ NormaliserRoom room;
   const int row = blockIdx.x;
   RowSlice<DT> s;
   s.init(p.student + static_cast<long long>(row) * p.stride * Elem<DT>::bytes, p.V, 0, p.share, p.seg, nullptr, 0);
-  wait_for_inputs();
-  const Statistics st = *statistics_of(p, row);
-  if (st.mass64 == 0.0) {
-    if (threadIdx.x == 0) p.loss[row] = 0.0f;
-    return;
+  const bool early = row < p.early;  // (the student is settled; whether the row has shares is known later)
+  Statistics st;
+  if (!early) {
+    wait_for_inputs();
+    st = *statistics_of(p, row);
+    if (st.mass64 == 0.0) {
+      if (threadIdx.x == 0) p.loss[row] = 0.0f;
+      return;
+    }
   }
   const float c = fminf(static_cast<float>(1.4426950408889634 / static_cast<double>(p.T)), 3e38f);
-  const f32x2 cc = pack2(c, c);
-  float m = -INFINITY;
-  double z = 0.0;
-  s.stream(s.begin + (threadIdx.x & 31), s.end, [&](const uint4& r) {
+  RunningSum<DT> sum;
+  s.stream(s.begin + (threadIdx.x & 31), s.end, [&](const uint4 (&r)[4]) {
     RunningMax<DT> top;
-    top.add(r);
-    const float t = top.value();
-    if (t > m || t != t) {  // (a maximum that is NaN stays it)
-      z *= static_cast<double>(m == -INFINITY ? 0.0f : ex2_approx((m - t) * c));
-      m = t;
-    }
-    if (m != -INFINITY) z += static_cast<double>(sum_exp2<DT>(r, pack2(-m, -m), cc));
-  });
-  float all = m;
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) all = max_nan(all, __shfl_xor_sync(0xffffffffu, all, d));
-  if (m != -INFINITY) z *= static_cast<double>(ex2_approx((m - all) * c));
-  const Normaliser n = row_normaliser(room, 1, 0, c, all, z);
+    for (int k = 0; k < 4; ++k) top.add(r[k]);
+    sum.add(r, top, c);
+  });
+  if (early) {
+    wait_for_inputs();
+    st = *statistics_of(p, row);
+    if (st.mass64 == 0.0) {
+      if (threadIdx.x == 0) p.loss[row] = 0.0f;
+      return;
+    }
+  }
+  float m = sum.m;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, d));
+  sum.to(m, c);
+  const Normaliser n = row_normaliser(room, 1, 0, c, m, sum.z);
   if (threadIdx.x == 0) finish_loss(p, row, st, n, true);
 }
 
@@ -435,7 +441,7 @@ cos_status distill(const cos_distill_args* a, void* cuda_stream) {
   p.seg = plan.seg;
   p.res = plan.res;
   p.early = 2 * plan.sms;
-  if (MODE == kLoss && a->rows >= 2 * plan.sms) plan_row(a->vocab, a->dtype, &p.share, &p.seg);
+  if (MODE == kLoss && a->rows >= plan.sms) plan_row(a->vocab, a->dtype, &p.share, &p.seg);
   p.lists = a->lists;
   p.k = a->k;
   p.ids = a->ids;
@@ -455,7 +461,7 @@ cos_status distill(const cos_distill_args* a, void* cuda_stream) {
       const cudaError_t first = slice_launch(cos_distill_shares_kernel<DT>, p, a->rows, 1, static_cast<size_t>(a->lists) * a->k * (sizeof(double) + sizeof(int)), stream, kShareThreads);
       if (first != cudaSuccess) return first;
     }
-    if (MODE == kLoss && a->rows >= 2 * plan.sms) return slice_launch(cos_distill_stream_kernel<DT>, p, a->rows, 1, 0, stream);
+    if (MODE == kLoss && a->rows >= plan.sms) return slice_launch(cos_distill_stream_kernel<DT>, p, a->rows, 1, 0, stream);
     return slice_launch(cos_distill_kernel<DT, MODE>, p, a->rows * plan.parts, MODE == kGrad ? 1 : plan.parts, plan.smem, stream);
   };
   e = a->dtype == COS_DTYPE_F32    ? launches(std::integral_constant<int, COS_DTYPE_F32>())

@@ -15,6 +15,8 @@
 // series of 2^r for |r| <= 2^-10 (the fourth term is below 1e-14), rounded to whole multiples of 2^-scale and summed as integers: a token is drawn where a
 // border of the cumulative sums lies next to u, and 32-bit sums are off by more than the weight of a token there.  Integers make sums independent of their
 // order, so atomics and the split over blocks change nothing.
+#include <float.h>
+
 #include "cos_slice.cuh"
 
 namespace cosv {
@@ -72,6 +74,9 @@ __device__ __forceinline__ int token_at(u64 place) { return static_cast<int>(0xf
 constexpr int kTable = 512;
 constexpr float kNear = 36.0f;
 
+struct Everything {
+  __device__ __forceinline__ bool operator()(float, int) const { return true; }
+};
 // exp((l - m) / T) in whole multiples of 2^-scale.
 template <int DT>
 struct Weight {
@@ -115,26 +120,43 @@ struct Weight {
   __device__ __forceinline__ u64 near(float l) const {  // below(l) < kNear; at most 2^46
     return static_cast<u64>(__double_as_longlong(exact(l) + 4503599627370496.0)) & 0xfffffffffffffull;
   }
-  __device__ __forceinline__ unsigned far(float x) const {  // x = below(l) >= kNear; at most 2^10
-    return __float_as_uint(ex2_approx(static_cast<float>(scale) - x) + 8388608.0f) - 0x4b000000u;
+  __device__ __forceinline__ unsigned far(float l) const {  // below(l) >= kNear; at most 2^10
+    return __float_as_uint(ex2_approx(fmaf(fmaf(-0.5f, l, half), -c32x2, static_cast<float>(scale))) + 8388608.0f) - 0x4b000000u;
   }
   // l is not +inf or NaN; 0 for -inf.
-  __device__ __forceinline__ u64 of(float l) const {
-    const float x = below(l);
-    return x < kNear ? near(l) : far(x);
+  __device__ __forceinline__ u64 of(float l) const { return below(l) < kNear ? near(l) : far(l); }
+  // ... of all entries of a vector, which are far.
+  __device__ __forceinline__ unsigned far_vector(const uint4& r) const {
+    f32x2 x[Elem<DT>::E / 2];
+    unpack_pairs<DT>(r, x);
+    const f32x2 minus_half = pack2(-0.5f, -0.5f), h = pack2(half, half), c = pack2(-c32x2, -c32x2), unit = pack2(static_cast<float>(scale), static_cast<float>(scale)), whole = pack2(8388608.0f, 8388608.0f);
+    unsigned sum = 0;
+#pragma unroll
+    for (int k = 0; k < Elem<DT>::E / 2; ++k) {
+      const f32x2 a = fma2(fma2(x[k], minus_half, h), c, unit);
+      const f32x2 w = add2(pack2(ex2_approx(lo2(a)), ex2_approx(hi2(a))), whole);
+      sum += __float_as_uint(lo2(w)) + __float_as_uint(hi2(w));
+    }
+    return sum - static_cast<unsigned>(Elem<DT>::E) * 0x4b000000u;
   }
   // Sum over the entries of a vector that keep(value, token) holds of.  Those far below the largest go by 32 bits, all at once; the others one by one (two under
   // way), by 64-bit instructions that take half the time of a sweep where most entries are near, and next to none where few are.
   template <class K>
   __device__ __forceinline__ u64 of_vector(const uint4& r, int token, K&& keep) const {
     constexpr int E = Elem<DT>::E;
+    constexpr bool kAll = std::is_same<std::decay_t<K>, Everything>::value;
+    if (kAll) {
+      RunningMax<DT> top;
+      top.add(r);
+      if (!(below(top.value()) < kNear)) return far_vector(r);
+    }
     unsigned tail = 0, head = 0;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      const float v = entry<DT>(r, e), x = below(v);
-      const bool kept = keep(v, token + e);
-      if (kept && x < kNear) head |= 1u << e;
-      tail += kept && x >= kNear ? far(x) : 0u;
+      const float v = entry<DT>(r, e);
+      const bool kept = keep(v, token + e), close = below(v) < kNear;
+      head |= static_cast<unsigned>(kept & close) << e;
+      tail += kept & !close ? far(v) : 0u;
     }
     u64 sum = tail;
     while (head) {
@@ -156,6 +178,29 @@ struct Weight {
     return __half2float(__ushort_as_half(static_cast<unsigned short>(h)));
   }
 };
+
+// How many entries are above -inf.
+template <int DT>
+__device__ __forceinline__ unsigned finite_entries(const uint4& r) {
+  unsigned low;
+  if constexpr (DT == COS_DTYPE_F32) {
+    low = __float_as_uint(fminf(fminf(__uint_as_float(r.x), __uint_as_float(r.y)), fminf(__uint_as_float(r.z), __uint_as_float(r.w))));
+  } else if constexpr (DT == COS_DTYPE_BF16) {
+    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&r);
+    const __nv_bfloat162 m = __hmin2(__hmin2(h[0], h[1]), __hmin2(h[2], h[3]));
+    low = *reinterpret_cast<const unsigned*>(&m);
+  } else {
+    const __half2* h = reinterpret_cast<const __half2*>(&r);
+    const __half2 m = __hmin2(__hmin2(h[0], h[1]), __hmin2(h[2], h[3]));
+    low = *reinterpret_cast<const unsigned*>(&m);
+  }
+  const uint4 m = make_uint4(low, 0, 0, 0);
+  if (fminf(entry<DT>(m, 0), DT == COS_DTYPE_F32 ? INFINITY : entry<DT>(m, 1)) > -INFINITY) return Elem<DT>::E;
+  unsigned n = 0;
+#pragma unroll
+  for (int e = 0; e < Elem<DT>::E; ++e) n += entry<DT>(r, e) > -INFINITY;
+  return n;
+}
 
 struct Found {
   u64 before_count, before_mass, count;
@@ -510,6 +555,9 @@ __device__ __forceinline__ u64 limit_by_mass(Row<H>& w, const RowSlice<DT>& s, c
     const bool few = f.count <= kCandidates;
     u64 above = 0, inside = 0;
     s.raw([&](int token, const uint4& r) {
+      RunningMax<DT> top;
+      top.add(r);
+      if (!(bin_at(top.value()) < lo + 1.0f) && f.bin < kBins - 1) return;  // (all of it lies behind the bin)
       above += weight.of_vector(r, token, [&](float v, int) { return bin_at(v) < lo; });
 #pragma unroll
       for (int e = 0; e < Elem<DT>::E; ++e) {
@@ -723,7 +771,8 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
     return want >= static_cast<double>(mass) ? mass : (want < 1.0 ? 1ull : static_cast<u64>(want));
   };
 
-  u64 last = place_of(-3.402823466e+38f, 0x7fffffff);  // the last place that is kept; nothing at -inf is
+  const u64 everything = place_of(-FLT_MAX, 0x7fffffff);
+  u64 last = everything;  // the last place that is kept; nothing at -inf is
   if (by_k || by_p) {
     // bins of 1/32 of a power of two of the weight where sums of weights are wanted, else of 1/64 of a logit
     const float per_half = by_p ? fminf(32.0f * weight.c32x2, 1e30f) : 128.0f;
@@ -744,7 +793,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
       u64 sum = 0, mass = 0;
       if (!by_k) {  // (everything is looked at for the total; the histogram is filled on the way, for rows that want it)
         s.raw([&](int token, const uint4& r) {
-          sum += weight.of_vector(r, token, [](float, int) { return true; });
+          sum += weight.of_vector(r, token, Everything());
 #pragma unroll
           for (int e = 0; e < Elem<DT>::E; ++e) {
             const float v = entry<DT>(r, e);
@@ -818,7 +867,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
       if (by_k) {
         u64 mine = 0;
         s.raw([&](int token, const uint4& r) {
-          mine += weight.of_vector(r, token, [&](float v, int t) { return v > -INFINITY && place_of(v, t) >= last; });
+          mine += weight.of_vector(r, token, [&](float v, int t) { return (v > -INFINITY) & (place_of(v, t) >= last); });
         });
         total = exchange<Add>(x, w.turn, parts, rank, mine).a;
       }
@@ -828,18 +877,26 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
   }
 
   // what is kept, in order of the index
-  const float last_logit = logit_at(last);
-  const int last_token = token_at(last);
-  const auto keeps = [&](float v, int token) { return v >= least && v >= last_logit && (v > last_logit || token <= last_token); };
-  u64 mine = 0, kept = 0;
-  if (own >= fmaxf(least, last_logit))
+  const float last_logit = logit_at(last), bound = fmaxf(least, last_logit);
+  const int last_token = least > last_logit ? 0x7fffffff : token_at(last);
+  const auto keeps = [&](float v, int token) { return (v > bound) | ((v == bound) & (token <= last_token)); };
+  u64 mine = 0;
+  unsigned kept = 0;
+  if (last == everything && bound == last_logit) {
     s.raw([&](int token, const uint4& r) {
-      mine += weight.of_vector(r, token, [&](float v, int t) {
-        const bool it = keeps(v, t);
-        kept += it;
-        return it;
-      });
+      mine += weight.of_vector(r, token, Everything());
+      kept += finite_entries<DT>(r);
     });
+  } else if (own >= bound) {
+    s.raw([&](int token, const uint4& r) {
+      RunningMax<DT> top;
+      top.add(r);
+      if (!(top.value() >= bound)) return;
+      mine += weight.of_vector(r, token, keeps);
+#pragma unroll
+      for (int e = 0; e < Elem<DT>::E; ++e) kept += keeps(entry<DT>(r, e), token + e);
+    });
+  }
   const int t = w.turn & 1;
   const Words all = exchange<Add, Add>(x, w.turn, parts, rank, mine, kept);
   const u64 goal = drawn(all.a);
@@ -896,7 +953,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
 
 // kStream: a block for each row, which goes by in registers; what has candidates in it is read again.
 template <int DT, int kList, bool kStream>
-__global__ void __launch_bounds__(kSliceThreads, kStream ? 3 : 2) cos_top_kernel(const TopParams p) {
+__global__ void __launch_bounds__(kSliceThreads, 2) cos_top_kernel(const TopParams p) {
   extern __shared__ uint4 smem[];
   Shared<kList>& h = *reinterpret_cast<Shared<kList>*>(smem);
   __shared__ Exchange x;
@@ -910,28 +967,26 @@ __global__ void __launch_bounds__(kSliceThreads, kStream ? 3 : 2) cos_top_kernel
   if (tid == 0) h.listed = 0;
   Row<Shared<kList>> w = {h, x, parts, rank, 0, 0};
   const float c = fminf(static_cast<float>(1.4426950408889634 / static_cast<double>(p.T)), 3e38f);
-  const f32x2 cc = pack2(c, c);
   const int half = (p.c.seg / 32 + kGroups - 1) / kGroups * 32;  // vectors of a warp's groups
   Groups groups;
-  float own[kGroups], mine = -INFINITY;  // the largest of this thread's groups, and of them
-  double sum = 0.0;                      // against `mine`
+  float own[kGroups], mine;  // the largest of this thread's groups, and of them
+  double sum = 0.0;
   if constexpr (kStream) {
+    RunningSum<DT> part;
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) {
       RunningMax<DT> group;
-      s.stream(s.begin + (tid & 31) + g * half, min(s.end, s.begin + (g + 1) * half), [&](const uint4& r) {
+      s.stream(s.begin + (tid & 31) + g * half, min(s.end, s.begin + (g + 1) * half), [&](const uint4 (&r)[4]) {
         RunningMax<DT> top;
-        top.add(r);
-        group.add(r);
-        const float t = top.value();
-        if (t > mine || t != t) {  // (a maximum that is NaN stays it)
-          sum *= static_cast<double>(mine == -INFINITY ? 0.0f : ex2_approx((mine - t) * c));
-          mine = t;
-        }
-        if (mine != -INFINITY) sum += static_cast<double>(sum_exp2<DT>(r, pack2(-mine, -mine), cc));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) top.add(r[k]);
+        group.add(top);
+        part.add(r, top, c);
       });
       own[g] = group.value();
     }
+    mine = part.m;
+    sum = part.z;
     group_range(h, groups, mine, own[0] == -INFINITY ? own[1] : own[1] == -INFINITY ? own[0] : fminf(own[0], own[1]));
   } else {
     s.start();
@@ -955,7 +1010,7 @@ __global__ void __launch_bounds__(kSliceThreads, kStream ? 3 : 2) cos_top_kernel
   if constexpr (kStream) {
     if (mine != -INFINITY) sum *= static_cast<double>(ex2_approx((mine - m) * c));
   } else {
-    const f32x2 minus_m = pack2(-m, -m);
+    const f32x2 minus_m = pack2(-m, -m), cc = pack2(c, c);
     s.raw([&](int, const uint4& r) { sum += static_cast<double>(sum_exp2<DT>(r, minus_m, cc)); });
   }
   int n = kList + 1;
@@ -1052,7 +1107,7 @@ cos_status launch_rows(P& p, int rows, int vocab, int dtype, int device, size_t 
   OnDevice on(device);
   if (on.error != cudaSuccess) return call_failed("cudaSetDevice", on.error);
   SlicePlan plan;
-  cudaError_t e = slice_plan(device, rows, vocab, dtype, 44 * 1024, true, &plan);
+  cudaError_t e = slice_plan(device, rows, vocab, dtype, 64 * 1024, true, &plan);
   if (e != cudaSuccess) return call_failed("device query", e);
   if (static_cast<long long>(rows) * plan.parts > 0x7fffffffll) return call_failed(COS_ERR_UNSUPPORTED, "too many rows for one launch");
   if (whole) {  // a block for each row, which stays in memory
@@ -1080,7 +1135,10 @@ cudaError_t slice_plan(int device, int rows, int vocab, int dtype, int most, boo
   const int E = dtype == COS_DTYPE_F32 ? 4 : 8, kept = most / 16;
   const long long all = (static_cast<long long>(vocab) + 2 * (E - 1)) / E;
   long long parts = 1;
-  while ((parts < kSliceParts || !cluster) && ((all + parts - 1) / parts > kept || (rows * parts < 2 * plan->sms && all / parts >= kSliceThreads))) parts *= 2;
+  while ((parts < kSliceParts || !cluster) && (all + parts - 1) / parts > kept) parts *= 2;
+  const long long places[5] = {0, 2 * plan->sms, 2 * plan->sms, 256, 192};  // for blocks of rows in 1, 2, 4, 8, 16
+  for (int two = 1; two <= 4; ++two)
+    if (parts == 1ll << (two - 1) && all / parts >= kSliceThreads && rows * parts * 2 <= places[two]) parts *= 2;
   plan->parts = static_cast<int>(parts);
   plan->share = static_cast<int>((all + parts - 1) / parts);
   plan->seg = static_cast<int>((plan->share + 32 * kSliceWarps - 1) / (32 * kSliceWarps) * 32);
@@ -1161,5 +1219,5 @@ extern "C" cos_status cos_top_logits(const cos_top_args* a, void* cuda_stream) {
   if (e != cudaSuccess) return call_failed("device query", e);
   using Few = std::integral_constant<int, kCandidates>;
   if (a->k > kMost<kCandidates>) return call(std::integral_constant<int, kTopCandidates>(), std::false_type());
-  return a->rows >= 2 * sms ? call(Few(), std::true_type()) : call(Few(), std::false_type());
+  return a->rows >= sms ? call(Few(), std::true_type()) : call(Few(), std::false_type());
 }

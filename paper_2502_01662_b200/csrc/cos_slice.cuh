@@ -48,6 +48,9 @@ struct RunningMax {
     top[0] = larger(top[0], larger(r.x, r.z));
     top[kLast] = larger(top[kLast], larger(r.y, r.w));
   }
+  __device__ __forceinline__ void add(const RunningMax& o) {
+    for (int i = 0; i < static_cast<int>(sizeof(top) / sizeof(top[0])); ++i) top[i] = larger(top[i], o.top[i]);
+  }
   __device__ __forceinline__ float value() const {
     if constexpr (DT == COS_DTYPE_F32) return max_nan(__uint_as_float(top[0]), __uint_as_float(top[1]));
     const uint4 r = make_uint4(top[0], 0, 0, 0);
@@ -68,6 +71,28 @@ __device__ __forceinline__ float sum_exp2(const uint4& r, f32x2 minus_m, f32x2 c
   }
   return lo2(sum) + hi2(sum);
 }
+
+// A lane's part of a softmax normaliser, against the largest entry it has seen.
+template <int DT>
+struct RunningSum {
+  float m = -INFINITY;
+  double z = 0.0;
+  __device__ __forceinline__ void to(float t, float c) {  // (a maximum that is NaN stays it)
+    if (t > m || t != t) {
+      z *= static_cast<double>(m == -INFINITY ? 0.0f : ex2_approx((m - t) * c));
+      m = t;
+    }
+  }
+  __device__ __forceinline__ void add(const uint4 (&r)[4], const RunningMax<DT>& top, float c) {
+    to(top.value(), c);
+    if (m == -INFINITY) return;
+    const f32x2 minus_m = pack2(-m, -m), cc = pack2(c, c);
+    float part = sum_exp2<DT>(r[0], minus_m, cc);
+#pragma unroll
+    for (int k = 1; k < 4; ++k) part += sum_exp2<DT>(r[k], minus_m, cc);
+    z += static_cast<double>(part);
+  }
+};
 
 template <int DT>
 struct RowSlice {
@@ -150,21 +175,28 @@ struct RowSlice {
       f(token(i), v);
     }
   }
-  // f(vector) for every vector of this lane in [from, to) of the slice, fetched from memory with several under way.
+  // f(four vectors) for the vectors of this lane from `from` on, before `to`, fetched from memory, the next four under way meanwhile (-inf where there are fewer).
   template <class F>
   __device__ __forceinline__ void stream(int from, int to, F&& f) const {
-    constexpr int kAhead = 4;
-    uint4 r[kAhead];
+    const int whole = static_cast<int>(min(static_cast<long long>(to), (static_cast<long long>(V) + off) / E - v0));  // vectors before it end inside the row
+    const auto get = [&](int i, uint4 (&r)[4]) {
+      if (i + 96 < whole && (v0 + i > 0 || off == 0)) {
+        const char* at = base + (static_cast<long long>(v0) + i) * 16;
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) r[k] = from + 32 * k < to ? fetch(from + 32 * k) : neg_inf_vector<DT>();
-    for (int i = from; i < to; i += 32 * kAhead) {
+        for (int k = 0; k < 4; ++k) r[k] = ldg_stream16(at + 512 * k);
+      } else {
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        const uint4 here = r[k];
-        const int next = i + 32 * (k + kAhead);
-        r[k] = next < to ? fetch(next) : neg_inf_vector<DT>();
-        f(here);
+        for (int k = 0; k < 4; ++k) r[k] = i + 32 * k < to ? fetch(i + 32 * k) : neg_inf_vector<DT>();
       }
+    };
+    uint4 a[4], b[4];
+    get(from, a);
+    for (int i = from; i < to; i += 256) {
+      get(i + 128, b);
+      f(a);
+      if (i + 128 >= to) break;
+      get(i + 256, a);
+      f(b);
     }
   }
   // f(token of the first entry, vector) likewise.
@@ -327,7 +359,8 @@ __device__ __forceinline__ Words exchange(Exchange& x, int& turn, int parts, int
 }
 
 // How a row is cut up: as few blocks as `most` bytes of shared memory each allow (16 at most: what does not fit is read again where it is wanted), or more where
-// that leaves multiprocessors without two blocks, down to a vector a thread.  cluster: the blocks are one (a power of two).
+// all of them still have their places side by side (two a multiprocessor; of clusters of 8 and 16 there are places for 32 and 12 or so, since one lies in a
+// group of 16 to 20 multiprocessors), down to a vector a thread.  cluster: the blocks are one (a power of two).
 struct SlicePlan {
   int parts, share, seg, res, sms;
   size_t smem;

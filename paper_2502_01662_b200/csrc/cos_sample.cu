@@ -72,7 +72,7 @@ __device__ __forceinline__ float logit_at(u64 place) { return unordered(static_c
 __device__ __forceinline__ int token_at(u64 place) { return static_cast<int>(0xffffffffu - static_cast<unsigned>(place)); }
 
 constexpr int kTable = 512;
-constexpr float kNear = 36.0f;
+constexpr double kNear = 36.0;  // powers of two
 
 struct Everything {
   __device__ __forceinline__ bool operator()(float, int) const { return true; }
@@ -81,6 +81,7 @@ struct Everything {
 template <int DT>
 struct Weight {
   float half, c32x2;    // half the row's largest logit (differences of halves do not overflow), twice log2(e) / T
+  float near_from;      // logits from here on go by 64 bits
   double m64, c;        // the logit, log2(e) / T
   const double* table;  // 2^(j / 512)
   int scale;
@@ -94,11 +95,10 @@ struct Weight {
     m64 = widen(m);
     c = 1.4426950408889634 / static_cast<double>(T);
     c32x2 = fmaxf(fminf(static_cast<float>(2.0 * c), 3e38f), 1e-37f);  // (-inf is infinitely far at any temperature)
+    near_from = fmaxf(static_cast<float>(m64 - kNear / c), -FLT_MAX);
     table = table_;
     scale = min(46, 63 - (32 - __clz(V - 1)));
   }
-  // Powers of two that l's weight is below the largest.
-  __device__ __forceinline__ float below(float l) const { return fmaf(-0.5f, l, half) * c32x2; }
   // 2^(i / 512) units
   __device__ __forceinline__ double power(int i) const {
     const double e = table[i & (kTable - 1)];
@@ -117,15 +117,15 @@ struct Weight {
     e *= table[n & (kTable - 1)];
     return __hiloint2double(__double2hiint(e) + (((n >> 9) + scale) << 20), __double2loint(e));
   }
-  __device__ __forceinline__ u64 near(float l) const {  // below(l) < kNear; at most 2^46
+  __device__ __forceinline__ u64 near(float l) const {  // l >= near_from; at most 2^46
     return static_cast<u64>(__double_as_longlong(exact(l) + 4503599627370496.0)) & 0xfffffffffffffull;
   }
-  __device__ __forceinline__ unsigned far(float l) const {  // below(l) >= kNear; at most 2^10
+  __device__ __forceinline__ unsigned far(float l) const {  // l < near_from: at most 2^10 (else some number)
     return __float_as_uint(ex2_approx(fmaf(fmaf(-0.5f, l, half), -c32x2, static_cast<float>(scale))) + 8388608.0f) - 0x4b000000u;
   }
   // l is not +inf or NaN; 0 for -inf.
-  __device__ __forceinline__ u64 of(float l) const { return below(l) < kNear ? near(l) : far(l); }
-  // ... of all entries of a vector, which are far.
+  __device__ __forceinline__ u64 of(float l) const { return l >= near_from ? near(l) : far(l); }
+  // The sum of far() of all entries of a vector, modulo 2^32.
   __device__ __forceinline__ unsigned far_vector(const uint4& r) const {
     f32x2 x[Elem<DT>::E / 2];
     unpack_pairs<DT>(r, x);
@@ -144,19 +144,28 @@ struct Weight {
   template <class K>
   __device__ __forceinline__ u64 of_vector(const uint4& r, int token, K&& keep) const {
     constexpr int E = Elem<DT>::E;
-    constexpr bool kAll = std::is_same<std::decay_t<K>, Everything>::value;
-    if (kAll) {
+    unsigned tail = 0, head = 0;
+    if constexpr (std::is_same<std::decay_t<K>, Everything>::value) {
+      tail = far_vector(r);
       RunningMax<DT> top;
       top.add(r);
-      if (!(below(top.value()) < kNear)) return far_vector(r);
-    }
-    unsigned tail = 0, head = 0;
+      if (top.value() < near_from) return tail;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const float v = entry<DT>(r, e);
-      const bool kept = keep(v, token + e), close = below(v) < kNear;
-      head |= static_cast<unsigned>(kept & close) << e;
-      tail += kept & !close ? far(v) : 0u;
+      for (int e = 0; e < E; ++e) {
+        const float v = entry<DT>(r, e);
+        if (v >= near_from) {
+          head |= 1u << e;
+          tail -= far(v);  // (it is not among these)
+        }
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float v = entry<DT>(r, e);
+        const bool kept = keep(v, token + e), close = v >= near_from;
+        head |= static_cast<unsigned>(kept & close) << e;
+        tail += kept & !close ? far(v) : 0u;
+      }
     }
     u64 sum = tail;
     while (head) {
@@ -218,7 +227,7 @@ struct Shared {
   Found found[2];
   u64 word[2];
   unsigned steps[64];
-  int listed, pad[3];
+  int listed, hits, pad[2];
 };
 using SampleShared = Shared<kCandidates>;
 static_assert(sizeof(SampleShared) % 16 == 0 && sizeof(Shared<kTopCandidates>) % 16 == 0, "the slice lies behind it");
@@ -350,11 +359,19 @@ template <int DT, class H>
 __device__ __forceinline__ void list_from(H& h, float from, int token, const uint4& r) {
   RunningMax<DT> top;
   top.add(r);
-  if (top.value() >= from)
-#pragma unroll 1
-    for (int e = 0; e < Elem<DT>::E; ++e) {
-      const float v = Weight<DT>::pick(r, e);
-      if (v >= from && v > -INFINITY) list(h, v, token + e);
+  if (!(top.value() >= from)) return;
+  unsigned in = 0;
+#pragma unroll
+  for (int e = 0; e < Elem<DT>::E; ++e) {
+    const float v = entry<DT>(r, e);
+    in |= static_cast<unsigned>((v >= from) & (v > -INFINITY)) << e;
+  }
+  if (in == 0) return;
+  int at = atomicAdd(&h.listed, __popc(in));
+  for (; in; in &= in - 1, ++at)
+    if (at < static_cast<int>(sizeof(h.list) / sizeof(u64))) {
+      const int e = __ffs(in) - 1;
+      h.list[at] = place_of(Weight<DT>::pick(r, e), token + e);
     }
 }
 // Behind the sweep that listed them (h.listed was 0): how many candidates the row has, and the sums over the row of `sum` and of the lanes' masses of what
@@ -964,7 +981,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_top_kernel(const TopPara
   RowSlice<DT> s;
   s.init(static_cast<const char*>(p.c.logits) + static_cast<long long>(row) * p.c.stride * Elem<DT>::bytes, p.c.V, rank, p.c.share, p.c.seg, smem + sizeof(h) / 16, p.c.res);
   if (tid < 64) h.steps[tid] = 0;
-  if (tid == 0) h.listed = 0;
+  if (tid == 0) h.listed = h.hits = 0;
   Row<Shared<kList>> w = {h, x, parts, rank, 0, 0};
   const float c = fminf(static_cast<float>(1.4426950408889634 / static_cast<double>(p.T)), 3e38f);
   const int half = (p.c.seg / 32 + kGroups - 1) / kGroups * 32;  // vectors of a warp's groups
@@ -1017,10 +1034,18 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_top_kernel(const TopPara
   if (p.k <= kHeadMost) {
     const float from = reached_by(h, groups, own, p.k);
     if constexpr (kStream) {
+// the groups with candidates are dealt out over the warps, whose lanes read a group's vectors side by side
+      unsigned short* const hit = reinterpret_cast<unsigned short*>(h.group);
 #pragma unroll
       for (int g = 0; g < kGroups; ++g)
-        if (own[g] >= from)
-          for (int i = s.begin + (tid & 31) + g * half; i < min(s.end, s.begin + (g + 1) * half); i += 32) list_from<DT>(h, from, s.token(i), s.fetch(i));
+        if (own[g] >= from) hit[atomicAdd(&h.hits, 1)] = static_cast<unsigned short>(tid * kGroups + g);
+      __syncthreads();
+      const int hits = h.hits;
+      for (int q = tid >> 5; q < hits; q += kSliceWarps) {
+        const int thread = hit[q] / kGroups, g = hit[q] % kGroups;
+        const int begin = min(s.nv, (thread >> 5) * p.c.seg), end = min(min(s.nv, begin + p.c.seg), begin + (g + 1) * half);
+        for (int i = begin + g * half + (thread & 31) + 32 * (tid & 31); i < end; i += 32 * 32) list_from<DT>(h, from, s.token(i), s.fetch(i));
+      }
     } else if (mine >= from) {
       s.raw([&](int token, const uint4& r) { list_from<DT>(h, from, token, r); });
     }

@@ -26,14 +26,15 @@ constexpr int kLoss = 0, kGrad = 1, kStep = 2, kShareThreads = 128;
 struct DistillParams {
   const char* student;
   long long stride;
-  int rows, V, parts, share, seg, res;
+  int rows, V, parts, shift, share, seg, res;  // parts: 2^shift
   int early;  // blocks that may start on their rows before the shares are there
   int lists, k;
   const int* ids;
   const float* values;
   const float* lse;
   float w[COS_MAX_MODELS];
-  float T;
+  float T, c;    // c = log2(e) / T
+  double inv_T;
   const float* row_weights;
   float* loss;
   float* statistics;
@@ -45,6 +46,7 @@ struct DistillParams {
 struct Shares {
   double* t;  // 0 for an empty entry
   int* id;
+  float* s;   // the student's logits there
   double *per_warp, *list_max, *list_sum;
 };
 
@@ -63,12 +65,18 @@ __device__ __forceinline__ double block_sum(double v, double* per_warp) {
   return s;
 }
 
+template <int DT>
+__device__ __forceinline__ float student_at(const char* row, int x) {
+  return Elem<DT>::load1(row, x);
+}
+
 // Every entry's share to shared memory (0 for an empty one); returns their sum, NaN where an entry names no token.
-__device__ __forceinline__ double row_shares(const DistillParams& p, int row, const Shares& sh) {
+template <int DT>
+__device__ __forceinline__ double row_shares(const DistillParams& p, const char* student, int row, const Shares& sh) {
   const int n = p.lists * p.k, tid = threadIdx.x;
   const int* ids = p.ids + static_cast<long long>(row) * n;
   const float* values = p.values + static_cast<long long>(row) * n;
-  const double inv_T = 1.0 / static_cast<double>(p.T);
+  const double inv_T = p.inv_T;
   if (!p.lse) {  // softmax over each list: a warp for each
     for (int g = tid >> 5; g < p.lists; g += kShareThreads / 32) {
       double m = -INFINITY, s = 0.0;
@@ -89,7 +97,7 @@ __device__ __forceinline__ double row_shares(const DistillParams& p, int row, co
   double mine = 0.0;
   for (int e = tid; e < n; e += kShareThreads) {
     const int id = ids[e], g = e / p.k;
-    const float v = values[e];
+    const float v = values[e], s = id >= 0 && id < p.V ? student_at<DT>(student, id) : 0.0f;
     double t = 0.0;
     if (id >= 0 && v != -INFINITY) {
       const double w = static_cast<double>(p.w[g]);
@@ -100,15 +108,11 @@ __device__ __forceinline__ double row_shares(const DistillParams& p, int row, co
       if (id >= p.V) t = __longlong_as_double(0x7ff8000000000000ll);
     }
     sh.id[e] = id;
+    sh.s[e] = s;
     sh.t[e] = t;
     mine += t;
   }
   return block_sum(mine, sh.per_warp);
-}
-
-template <int DT>
-__device__ __forceinline__ float student_at(const char* row, int x) {
-  return Elem<DT>::load1(row, x);
 }
 
 template <int DT>
@@ -240,17 +244,17 @@ __global__ void __launch_bounds__(kShareThreads) cos_distill_shares_kernel(const
   wait_for_inputs();
   asm volatile("griddepcontrol.launch_dependents;");  // (the rows: they read the student, which is settled where every block has come here)
   const int row = blockIdx.x, n = p.lists * p.k;
-  const Shares sh = {reinterpret_cast<double*>(smem), reinterpret_cast<int*>(smem) + 2 * n, per_warp, list_max, list_sum};
-  const double mass = row_shares(p, row, sh);
+  const Shares sh = {reinterpret_cast<double*>(smem), reinterpret_cast<int*>(smem) + 2 * n, reinterpret_cast<float*>(smem) + 3 * n, per_warp, list_max, list_sum};
+  const char* student = p.student + static_cast<long long>(row) * p.stride * Elem<DT>::bytes;
+  const double mass = row_shares<DT>(p, student, row, sh);
   if (!(mass != 0.0)) {  // nothing to learn from
     if (threadIdx.x == 0) *statistics_of(p, row) = {0.0f, 0.0f, 0.0f, 0.0f, 0.0, 0.0};
     return;
   }
-  const char* student = p.student + static_cast<long long>(row) * p.stride * Elem<DT>::bytes;
   int at = 0;
   while (at < n && !(sh.t[at] != 0.0 && sh.id[at] < p.V)) ++at;
-  const float ref = at < n ? student_at<DT>(student, sh.id[at]) : 0.0f;
-  const double base = fabsf(ref) < INFINITY ? static_cast<double>(ref) : 0.0, inv_T = 1.0 / static_cast<double>(p.T);
+  const float ref = at < n ? sh.s[at] : 0.0f;
+  const double base = fabsf(ref) < INFINITY ? static_cast<double>(ref) : 0.0, inv_T = p.inv_T;
   float* const shares = shares_of(p, row);
   double listed = 0.0;
   for (int e = threadIdx.x; e < n; e += kShareThreads) {
@@ -265,7 +269,7 @@ __global__ void __launch_bounds__(kShareThreads) cos_distill_shares_kernel(const
           t += sh.t[j];
         }
       if (!first) t = 0.0;
-      if (t != 0.0) listed += t * (log(t) - (static_cast<double>(student_at<DT>(student, id)) - base) * inv_T);
+      if (t != 0.0) listed += t * (log(t) - (static_cast<double>(sh.s[e]) - base) * inv_T);
     }
     shares[e] = static_cast<float>(t);
   }
@@ -273,9 +277,9 @@ __global__ void __launch_bounds__(kShareThreads) cos_distill_shares_kernel(const
   if (threadIdx.x == 0) *statistics_of(p, row) = {0.0f, 0.0f, static_cast<float>(mass), static_cast<float>(base), listed, mass};
 }
 
-__device__ __forceinline__ float log2_of(const Normaliser& z) { return z.m == -INFINITY ? __int_as_float(0x7fc00000) : static_cast<float>(log2(z.z)); }
+__device__ __forceinline__ float log2_of(const Normaliser& z) { return z.m == -INFINITY ? __int_as_float(0x7fc00000) : log2f(static_cast<float>(z.z)); }
 __device__ __forceinline__ void finish_loss(const DistillParams& p, int row, const Statistics& st, const Normaliser& z, bool keep) {
-  const double inv_T = 1.0 / static_cast<double>(p.T);
+  const double inv_T = p.inv_T;
   const float log_z = log2_of(z);
   p.loss[row] = z.m == -INFINITY ? log_z : static_cast<float>(st.listed + st.mass64 * ((static_cast<double>(z.m) - static_cast<double>(st.reference)) * inv_T + log(z.z)));
   if (keep) {
@@ -301,7 +305,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_distill_stream_kernel(co
       return;
     }
   }
-  const float c = fminf(static_cast<float>(1.4426950408889634 / static_cast<double>(p.T)), 3e38f);
+  const float c = p.c;
   RunningSum<DT> sum;
   s.stream(s.begin + (threadIdx.x & 31), s.end, [&](const uint4 (&r)[4]) {
     RunningMax<DT> top;
@@ -330,7 +334,7 @@ template <int DT, int MODE>
 __global__ void __launch_bounds__(kSliceThreads, 3) cos_distill_kernel(const DistillParams p) {
   extern __shared__ uint4 smem[];
   __shared__ NormaliserRoom room;
-  const int parts = p.parts, rank = blockIdx.x % parts, row = blockIdx.x / parts, tid = threadIdx.x, n = p.lists * p.k;
+  const int parts = p.parts, rank = blockIdx.x & (parts - 1), row = blockIdx.x >> p.shift, tid = threadIdx.x, n = p.lists * p.k;
   const bool wide = MODE != kGrad && parts > 1;
   if (wide) cluster_barrier_arrive();
   const char* student = p.student + static_cast<long long>(row) * p.stride * Elem<DT>::bytes;
@@ -370,7 +374,7 @@ __global__ void __launch_bounds__(kSliceThreads, 3) cos_distill_kernel(const Dis
     }
   }
   s.finish();
-  const float c = fminf(static_cast<float>(1.4426950408889634 / static_cast<double>(p.T)), 3e38f);
+  const float c = p.c;
   float m = st.m, log_z = st.log_z;
   if (MODE != kGrad) {
     if (wide) cluster_barrier_wait();  // (every block of the row has started)
@@ -386,7 +390,7 @@ __global__ void __launch_bounds__(kSliceThreads, 3) cos_distill_kernel(const Dis
       write_slice<DT>(s, grad, false, [](const uint4& nothing) { return nothing; });
       return;
     }
-    const double per = static_cast<double>(weight) / static_cast<double>(p.T), mass = static_cast<double>(st.mass);
+    const double per = static_cast<double>(weight) * p.inv_T, mass = static_cast<double>(st.mass);
     const float scale = static_cast<float>(per * mass);
     const f32x2 scales = pack2(scale, scale), minus_m = pack2(-m, -m), cc = pack2(c, c), minus_log_z = pack2(-log_z, -log_z);
     write_slice<DT>(s, grad, true, [&](const uint4& r) { return gradient_of<DT>(r, scales, minus_m, cc, minus_log_z); });
@@ -437,6 +441,7 @@ cos_status distill(const cos_distill_args* a, void* cuda_stream) {
   p.rows = a->rows;
   p.V = a->vocab;
   p.parts = plan.parts;
+  p.shift = __builtin_ctz(plan.parts);
   p.share = plan.share;
   p.seg = plan.seg;
   p.res = plan.res;
@@ -449,6 +454,8 @@ cos_status distill(const cos_distill_args* a, void* cuda_stream) {
   p.lse = a->lse;
   for (int g = 0; g < a->lists; ++g) p.w[g] = a->weights[g];
   p.T = a->temperature;
+  p.c = fminf(static_cast<float>(1.4426950408889634 / static_cast<double>(p.T)), 3e38f);
+  p.inv_T = 1.0 / static_cast<double>(p.T);
   p.row_weights = a->row_weights;
   p.loss = a->loss;
   p.statistics = a->statistics;
@@ -458,7 +465,7 @@ cos_status distill(const cos_distill_args* a, void* cuda_stream) {
     constexpr int DT = decltype(dt)::value;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (MODE != kGrad) {
-      const cudaError_t first = slice_launch(cos_distill_shares_kernel<DT>, p, a->rows, 1, static_cast<size_t>(a->lists) * a->k * (sizeof(double) + sizeof(int)), stream, kShareThreads);
+      const cudaError_t first = slice_launch(cos_distill_shares_kernel<DT>, p, a->rows, 1, static_cast<size_t>(a->lists) * a->k * (sizeof(double) + sizeof(int) + sizeof(float)), stream, kShareThreads);
       if (first != cudaSuccess) return first;
     }
     if (MODE == kLoss && a->rows >= plan.sms) return slice_launch(cos_distill_stream_kernel<DT>, p, a->rows, 1, 0, stream);

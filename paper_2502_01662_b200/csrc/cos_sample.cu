@@ -26,6 +26,8 @@ constexpr int kBins = 1024, kBinBits = 10, kCandidates = 512, kTopCandidates = C
 // the largest k that a list of that size is used for
 template <int kList>
 constexpr int kMost = kList == kTopCandidates ? COS_TOP_MAX : 288;
+// A block of so few entries counts those of a bin, and adds up their places in it (in eighths), in one word.
+constexpr int kPackedEntries = 16384, kPackedShift = 17;
 constexpr int kFew = 128;
 constexpr int kHeadMost = kMost<kCandidates>, kHeadGuess = 96;  // the largest top-k that the head is tried for; the k it is tried with for a top-p alone
 static_assert(kCandidates == kSliceThreads, "a thread for each");
@@ -33,7 +35,7 @@ static_assert(kCandidates == kSliceThreads, "a thread for each");
 struct Common {  // of both kernels
   const void* logits;
   long long stride;
-  int V, parts, share, seg, res;
+  int V, parts, shift, share, seg, res;  // parts: 2^shift
 };
 
 struct SampleParams {
@@ -54,7 +56,7 @@ struct SampleParams {
 struct TopParams {
   Common c;
   int k;
-  float T;
+  float T, scale;  // scale = log2(e) / T
   float* values;
   int* ids;
   float* lse;
@@ -73,120 +75,6 @@ __device__ __forceinline__ int token_at(u64 place) { return static_cast<int>(0xf
 
 constexpr int kTable = 512;
 constexpr double kNear = 36.0;  // powers of two
-
-struct Everything {
-  __device__ __forceinline__ bool operator()(float, int) const { return true; }
-};
-// exp((l - m) / T) in whole multiples of 2^-scale.
-template <int DT>
-struct Weight {
-  float half, c32x2;    // half the row's largest logit (differences of halves do not overflow), twice log2(e) / T
-  float near_from;      // logits from here on go by 64 bits
-  double m64, c;        // the logit, log2(e) / T
-  const double* table;  // 2^(j / 512)
-  int scale;
-  // A finite float widened (0 and subnormal numbers to next to nothing): integer instructions, of which there are eight times as many a clock as conversions.
-  static __device__ __forceinline__ double widen(float v) {
-    const unsigned u = __float_as_uint(v);
-    return __hiloint2double(static_cast<int>((((u & 0x7fffffffu) >> 3) + 0x38000000u) | (u & 0x80000000u)), DT == COS_DTYPE_F32 ? static_cast<int>(u << 29) : 0);
-  }
-  __device__ __forceinline__ void init(float m, float T, int V, const double* table_) {
-    half = 0.5f * m;
-    m64 = widen(m);
-    c = 1.4426950408889634 / static_cast<double>(T);
-    c32x2 = fmaxf(fminf(static_cast<float>(2.0 * c), 3e38f), 1e-37f);  // (-inf is infinitely far at any temperature)
-    near_from = fmaxf(static_cast<float>(m64 - kNear / c), -FLT_MAX);
-    table = table_;
-    scale = min(46, 63 - (32 - __clz(V - 1)));
-  }
-  // 2^(i / 512) units
-  __device__ __forceinline__ double power(int i) const {
-    const double e = table[i & (kTable - 1)];
-    return __hiloint2double(__double2hiint(e) + (((i >> 9) + scale) << 20), __double2loint(e));
-  }
-  // Not rounded to the unit; l is at most 2^40 units of the temperature below the largest.
-  __device__ __forceinline__ double exact(float l) const {
-    constexpr double kRound = 13194139533312.0;  // 1.5 * 2^43: sums with it are multiples of 2^-9
-    const double d = widen(l) - m64;
-    const double k = fma(d, c, kRound);
-    const double r = fma(d, c, kRound - k);
-    const int n = __double2loint(k);
-    double e = fma(0.05550410866482158, r, 0.2402265069591007);  // ln(2)^i / i!
-    e = fma(e, r, 0.6931471805599453);
-    e = fma(e, r, 1.0);
-    e *= table[n & (kTable - 1)];
-    return __hiloint2double(__double2hiint(e) + (((n >> 9) + scale) << 20), __double2loint(e));
-  }
-  __device__ __forceinline__ u64 near(float l) const {  // l >= near_from; at most 2^46
-    return static_cast<u64>(__double_as_longlong(exact(l) + 4503599627370496.0)) & 0xfffffffffffffull;
-  }
-  __device__ __forceinline__ unsigned far(float l) const {  // l < near_from: at most 2^10 (else some number)
-    return __float_as_uint(ex2_approx(fmaf(fmaf(-0.5f, l, half), -c32x2, static_cast<float>(scale))) + 8388608.0f) - 0x4b000000u;
-  }
-  // l is not +inf or NaN; 0 for -inf.
-  __device__ __forceinline__ u64 of(float l) const { return l >= near_from ? near(l) : far(l); }
-  // The sum of far() of all entries of a vector, modulo 2^32.
-  __device__ __forceinline__ unsigned far_vector(const uint4& r) const {
-    f32x2 x[Elem<DT>::E / 2];
-    unpack_pairs<DT>(r, x);
-    const f32x2 minus_half = pack2(-0.5f, -0.5f), h = pack2(half, half), c = pack2(-c32x2, -c32x2), unit = pack2(static_cast<float>(scale), static_cast<float>(scale)), whole = pack2(8388608.0f, 8388608.0f);
-    unsigned sum = 0;
-#pragma unroll
-    for (int k = 0; k < Elem<DT>::E / 2; ++k) {
-      const f32x2 a = fma2(fma2(x[k], minus_half, h), c, unit);
-      const f32x2 w = add2(pack2(ex2_approx(lo2(a)), ex2_approx(hi2(a))), whole);
-      sum += __float_as_uint(lo2(w)) + __float_as_uint(hi2(w));
-    }
-    return sum - static_cast<unsigned>(Elem<DT>::E) * 0x4b000000u;
-  }
-  // Sum over the entries of a vector that keep(value, token) holds of.  Those far below the largest go by 32 bits, all at once; the others one by one (two under
-  // way), by 64-bit instructions that take half the time of a sweep where most entries are near, and next to none where few are.
-  template <class K>
-  __device__ __forceinline__ u64 of_vector(const uint4& r, int token, K&& keep) const {
-    constexpr int E = Elem<DT>::E;
-    unsigned tail = 0, head = 0;
-    if constexpr (std::is_same<std::decay_t<K>, Everything>::value) {
-      tail = far_vector(r);
-      RunningMax<DT> top;
-      top.add(r);
-      if (top.value() < near_from) return tail;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float v = entry<DT>(r, e);
-        if (v >= near_from) {
-          head |= 1u << e;
-          tail -= far(v);  // (it is not among these)
-        }
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float v = entry<DT>(r, e);
-        const bool kept = keep(v, token + e), close = v >= near_from;
-        head |= static_cast<unsigned>(kept & close) << e;
-        tail += kept & !close ? far(v) : 0u;
-      }
-    }
-    u64 sum = tail;
-    while (head) {
-      const int a = __ffs(head) - 1;
-      head &= head - 1;
-      const int b = head ? __ffs(head) - 1 : -1;
-      head &= head - 1;
-      const u64 wa = near(pick(r, a)), wb = near(pick(r, b < 0 ? a : b));
-      sum += wa + (b < 0 ? 0ull : wb);
-    }
-    return sum;
-  }
-  static __device__ __forceinline__ float pick(const uint4& r, int e) {
-    const int i = DT == COS_DTYPE_F32 ? e : e >> 1;
-    const unsigned lo = (i & 1) ? r.y : r.x, hi = (i & 1) ? r.w : r.z, w = (i & 2) ? hi : lo;
-    if (DT == COS_DTYPE_F32) return __uint_as_float(w);
-    const unsigned h = (e & 1) ? w >> 16 : w & 0xffffu;
-    if (DT == COS_DTYPE_BF16) return __uint_as_float(h << 16);
-    return __half2float(__ushort_as_half(static_cast<unsigned short>(h)));
-  }
-};
 
 // How many entries are above -inf.
 template <int DT>
@@ -210,6 +98,153 @@ __device__ __forceinline__ unsigned finite_entries(const uint4& r) {
   for (int e = 0; e < Elem<DT>::E; ++e) n += entry<DT>(r, e) > -INFINITY;
   return n;
 }
+
+// exp((l - m) / T) in whole multiples of 2^-scale.
+template <int DT>
+struct Weight {
+  float half, c32x2;    // half the row's largest logit (differences of halves do not overflow), twice log2(e) / T
+  float near_from;      // logits from here on go by 64 bits
+  double m64, c;        // the logit, log2(e) / T
+  const double* table;  // 2^(j / 512) in units
+  int scale;
+  // A finite float widened (0 and subnormal numbers to next to nothing): integer instructions, of which there are eight times as many a clock as conversions.
+  static __device__ __forceinline__ double widen(float v) {
+    const unsigned u = __float_as_uint(v);
+    return __hiloint2double(static_cast<int>((((u & 0x7fffffffu) >> 3) + 0x38000000u) | (u & 0x80000000u)), DT == COS_DTYPE_F32 ? static_cast<int>(u << 29) : 0);
+  }
+  __device__ __forceinline__ void init(float m, float T, int V, const double* table_) {
+    half = 0.5f * m;
+    m64 = widen(m);
+    c = 1.4426950408889634 / static_cast<double>(T);
+    c32x2 = fmaxf(fminf(static_cast<float>(2.0 * c), 3e38f), 1e-37f);  // (-inf is infinitely far at any temperature)
+    near_from = fmaxf(static_cast<float>(m64 - kNear / c), -FLT_MAX);
+    table = table_;
+    scale = scale_of(V);
+  }
+  static __device__ __forceinline__ int scale_of(int V) { return min(46, 63 - (32 - __clz(V - 1))); }
+  // 2^(i / 512) units
+  __device__ __forceinline__ double power(int i) const {
+    const double e = table[i & (kTable - 1)];
+    return __hiloint2double(__double2hiint(e) + (i >> 9 << 20), __double2loint(e));
+  }
+  // Not rounded to the unit; l is at most 2^40 units of the temperature below the largest.
+  __device__ __forceinline__ double exact(float l) const {
+    constexpr double kRound = 13194139533312.0;  // 1.5 * 2^43: sums with it are multiples of 2^-9
+    const double d = widen(l) - m64;
+    const double k = fma(d, c, kRound);
+    const double r = fma(d, c, kRound - k);
+    const int n = __double2loint(k);
+    double e = fma(0.05550410866482158, r, 0.2402265069591007);  // ln(2)^i / i!
+    e = fma(e, r, 0.6931471805599453);
+    e = fma(e, r, 1.0);
+    e *= table[n & (kTable - 1)];
+    return __hiloint2double(__double2hiint(e) + (n >> 9 << 20), __double2loint(e));
+  }
+  // l >= near_from; at most 2^46: the rounded number's bits, with kUnits above them
+  static constexpr u64 kUnits = 0x4330000000000000ull;
+  __device__ __forceinline__ u64 near_bits(float l) const { return static_cast<u64>(__double_as_longlong(exact(l) + 4503599627370496.0)); }
+  __device__ __forceinline__ u64 near(float l) const { return near_bits(l) - kUnits; }
+  __device__ __forceinline__ unsigned far(float l) const {  // l < near_from: at most 2^10 (else some number)
+    return __float_as_uint(ex2_approx(fmaf(fmaf(-0.5f, l, half), -c32x2, static_cast<float>(scale))) + 8388608.0f) - 0x4b000000u;
+  }
+  // l is not +inf or NaN; 0 for -inf.
+  __device__ __forceinline__ u64 of(float l) const { return l >= near_from ? near(l) : far(l); }
+  // The sum of far() of all entries of a vector, modulo 2^32.
+  __device__ __forceinline__ unsigned far_vector(const uint4& r) const {
+    f32x2 x[Elem<DT>::E / 2];
+    unpack_pairs<DT>(r, x);
+    const f32x2 minus_half = pack2(-0.5f, -0.5f), h = pack2(half, half), c = pack2(-c32x2, -c32x2), unit = pack2(static_cast<float>(scale), static_cast<float>(scale)), whole = pack2(8388608.0f, 8388608.0f);
+    unsigned sum = 0;
+#pragma unroll
+    for (int k = 0; k < Elem<DT>::E / 2; ++k) {
+      const f32x2 a = fma2(fma2(x[k], minus_half, h), c, unit);
+      const f32x2 w = add2(pack2(ex2_approx(lo2(a)), ex2_approx(hi2(a))), whole);
+      sum += __float_as_uint(lo2(w)) + __float_as_uint(hi2(w));
+    }
+    return sum - static_cast<unsigned>(Elem<DT>::E) * 0x4b000000u;
+  }
+  // The near entries of a vector that `head` has bits of (two under way), and what far() made of them.
+  __device__ __forceinline__ u64 near_ones(const uint4& r, unsigned head, unsigned& as_far) const {
+    u64 sum = 0;
+    while (head) {
+      const int a = __ffs(head) - 1;
+      head &= head - 1;
+      const bool two = head != 0;
+      const int b = two ? __ffs(head) - 1 : a;
+      head &= head - 1;
+      const float va = pick(r, a), vb = pick(r, b);
+      const u64 wa = near(va), wb = near(vb);
+      sum += wa + (two ? wb : 0ull);
+      as_far += far(va) + (two ? far(vb) : 0u);
+    }
+    return sum;
+  }
+  // Sum over the entries of a vector that keep(value, token) holds of.
+  template <class K>
+  __device__ __forceinline__ u64 of_vector(const uint4& r, int token, K&& keep) const {
+    unsigned kept = 0, close = 0;
+#pragma unroll
+    for (int e = 0; e < Elem<DT>::E; ++e) {
+      const float v = entry<DT>(r, e);
+      kept |= static_cast<unsigned>(keep(v, token + e)) << e;
+      close |= static_cast<unsigned>(v >= near_from) << e;
+    }
+    return of_some(r, kept, close);
+  }
+  // ... that `kept` has bits of, `close` of the near ones.
+  __device__ __forceinline__ u64 of_some(const uint4& r, unsigned kept, unsigned close) const {
+    unsigned unused = 0;
+    u64 sum = near_ones(r, kept & close, unused);
+    for (unsigned e = kept & ~close; e; e &= e - 1) sum += far(pick(r, __ffs(e) - 1));
+    return sum;
+  }
+  // Sum over all entries of this lane.  Those far below the largest go by 32 bits, all at once (near ones among them, modulo 2^32, and are taken off again); the near ones
+  // by 64-bit instructions in a second pass, in which every lane goes from one of its vectors with any to the next: few where the tail is long, and half the
+  // time of the sweep where most entries are near.
+  __device__ __forceinline__ u64 of_all(const RowSlice<DT>& s, unsigned& finite) const {
+    const int first = s.begin + (threadIdx.x & 31);
+    u64 sum = 0;
+    unsigned tail = 0;
+    for (int block = first; block < s.end; block += 32 * 32) {  // (a bit for each of 32 vectors)
+      unsigned any = 0;
+      const int end = min(s.end, block + 32 * 32);
+#pragma unroll 2
+      for (int i = block, bit = 0; i < end; i += 32, ++bit) {
+        const uint4 r = s.at(i);
+        RunningMax<DT> top;
+        top.add(r);
+        tail += far_vector(r);
+        finite += finite_entries<DT>(r);
+        any |= static_cast<unsigned>(top.value() >= near_from) << bit;
+      }
+      for (; any; any &= any - 1) {
+        const uint4 r = s.at(block + 32 * (__ffs(any) - 1));
+        unsigned head = 0, as_far = 0;
+#pragma unroll
+        for (int e = 0; e < Elem<DT>::E; ++e) head |= static_cast<unsigned>(entry<DT>(r, e) >= near_from) << e;
+        if (head == (1u << Elem<DT>::E) - 1) {
+          u64 bits = 0;
+#pragma unroll
+          for (int e = 0; e < Elem<DT>::E; ++e) bits += near_bits(entry<DT>(r, e));
+          sum += bits - Elem<DT>::E * kUnits;
+          as_far = far_vector(r);
+        } else {
+          sum += near_ones(r, head, as_far);
+        }
+        tail -= as_far;
+      }
+    }
+    return sum + tail;
+  }
+  static __device__ __forceinline__ float pick(const uint4& r, int e) {
+    const int i = DT == COS_DTYPE_F32 ? e : e >> 1;
+    const unsigned lo = (i & 1) ? r.y : r.x, hi = (i & 1) ? r.w : r.z, w = (i & 2) ? hi : lo;
+    if (DT == COS_DTYPE_F32) return __uint_as_float(w);
+    const unsigned h = (e & 1) ? w >> 16 : w & 0xffffu;
+    if (DT == COS_DTYPE_BF16) return __uint_as_float(h << 16);
+    return __half2float(__ushort_as_half(static_cast<unsigned short>(h)));
+  }
+};
 
 struct Found {
   u64 before_count, before_mass, count;
@@ -256,7 +291,7 @@ __device__ __forceinline__ void clear_bins(H& h) {
 // Behind the sweep that filled the blocks' bins and a barrier of the row: the sums over the blocks, in order, with mass_of(bin, count, lo, hi) for a bin.  The
 // bins may be cleared afterwards.
 template <class H, class M>
-__device__ __forceinline__ void merge_bins(Row<H>& w, bool masses, bool wide, Bins& b, M&& mass_of) {
+__device__ __forceinline__ void merge_bins(Row<H>& w, bool masses, bool wide, bool packed, Bins& b, M&& mass_of) {
   const int own = kBins / w.parts, each = own > kSliceThreads ? own / kSliceThreads : 1;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   b.n = tid * each < own ? each : 0;
@@ -272,17 +307,27 @@ __device__ __forceinline__ void merge_bins(Row<H>& w, bool masses, bool wide, Bi
       unsigned hi = 0;
       if (w.parts == 1) {
         n = w.h.count[i];
-        lo = w.h.lo[i];
+        lo = packed ? n & ((1u << kPackedShift) - 1) : w.h.lo[i];
         hi = w.h.hi[i];
+        if (packed) n >>= kPackedShift;
       } else {
+        for (int first = 0; first < w.parts; first += 8) {  // (eight blocks' under way at once, a block again where there are fewer)
+          unsigned each[8], low[8], high[8];
 #pragma unroll
-        for (int r = 0; r < kSliceParts; ++r)  // (all under way at once)
-          if (r < w.parts) {
-            const H* o = of_rank(&w.h, r);
-            n += o->count[i];
-            if (masses) lo += o->lo[i];
-            if (wide) hi += o->hi[i];
+          for (int r = 0; r < 8; ++r) {
+            const H* o = of_rank(&w.h, min(first + r, w.parts - 1));
+            each[r] = o->count[i];
+            low[r] = masses && !packed ? o->lo[i] : 0u;
+            high[r] = wide ? o->hi[i] : 0u;
           }
+#pragma unroll
+          for (int r = 0; r < 8; ++r)
+            if (first + r < w.parts) {
+              n += packed ? each[r] >> kPackedShift : each[r];
+              lo += packed ? each[r] & ((1u << kPackedShift) - 1) : low[r];
+              hi += high[r];
+            }
+        }
       }
       b.count[q] = n;
       if (masses) b.mass[q] = mass_of(i, n, lo, hi);
@@ -354,25 +399,26 @@ __device__ __forceinline__ void list(H& h, float v, int token) {
   const int at = atomicAdd(&h.listed, 1);
   if (at < static_cast<int>(sizeof(h.list) / sizeof(u64))) h.list[at] = place_of(v, token);
 }
-// ... those of a vector from a logit on.
+// ... those of a vector from a logit on; a bit for each.
 template <int DT, class H>
-__device__ __forceinline__ void list_from(H& h, float from, int token, const uint4& r) {
+__device__ __forceinline__ unsigned list_from(H& h, float from, int token, const uint4& r) {
   RunningMax<DT> top;
   top.add(r);
-  if (!(top.value() >= from)) return;
+  if (!(top.value() >= from)) return 0;
   unsigned in = 0;
 #pragma unroll
   for (int e = 0; e < Elem<DT>::E; ++e) {
     const float v = entry<DT>(r, e);
     in |= static_cast<unsigned>((v >= from) & (v > -INFINITY)) << e;
   }
-  if (in == 0) return;
+  if (in == 0) return 0;
   int at = atomicAdd(&h.listed, __popc(in));
-  for (; in; in &= in - 1, ++at)
+  for (unsigned left = in; left; left &= left - 1, ++at)
     if (at < static_cast<int>(sizeof(h.list) / sizeof(u64))) {
-      const int e = __ffs(in) - 1;
+      const int e = __ffs(left) - 1;
       h.list[at] = place_of(Weight<DT>::pick(r, e), token + e);
     }
+  return in;
 }
 // Behind the sweep that listed them (h.listed was 0): how many candidates the row has, and the sums over the row of `sum` and of the lanes' masses of what
 // they listed.
@@ -447,7 +493,7 @@ __device__ __forceinline__ Range narrow(Row<H>& w, const S& s, W&& weight, bool 
     });
     row_barrier(w.parts);
     Bins b;
-    merge_bins(w, by_mass, by_mass, b, [](int, unsigned, u64 lo, unsigned hi) { return (static_cast<u64>(hi) << 32) + lo; });
+    merge_bins(w, by_mass, by_mass, false, b, [](int, unsigned, u64 lo, unsigned hi) { return (static_cast<u64>(hi) << 32) + lo; });
     const Found sub = locate(w, b, by_mass, target - (by_mass ? g.before_mass : g.before_count));
     g.before_count += sub.before_count;
     g.before_mass += sub.before_mass;
@@ -568,21 +614,28 @@ __device__ __forceinline__ u64 limit_by_mass(Row<H>& w, const RowSlice<DT>& s, c
   int n;
   for (;;) {  // the estimates are good to 1e-4: the bin is this one or one next to it
     const auto in = [&](float v) { return min(static_cast<int>(bin_at(v)), kBins - 1) == f.bin; };
-    const float lo = static_cast<float>(f.bin);
+    const float lo = static_cast<float>(f.bin), hi = lo + 1.0f;
+    const bool last_bin = f.bin == kBins - 1;
     const bool few = f.count <= kCandidates;
     u64 above = 0, inside = 0;
     s.raw([&](int token, const uint4& r) {
       RunningMax<DT> top;
       top.add(r);
-      if (!(bin_at(top.value()) < lo + 1.0f) && f.bin < kBins - 1) return;  // (all of it lies behind the bin)
-      above += weight.of_vector(r, token, [&](float v, int) { return bin_at(v) < lo; });
+      if (!(bin_at(top.value()) < hi) && !last_bin) return;  // (all of it lies behind the bin)
+      unsigned before = 0, here = 0, close = 0;
 #pragma unroll
       for (int e = 0; e < Elem<DT>::E; ++e) {
-        const float v = entry<DT>(r, e);
-        if (v > -INFINITY && in(v)) {
-          inside += weigh(v);
-          if (few) list(w.h, v, token + e);
-        }
+        const float v = entry<DT>(r, e), at = bin_at(v);
+        before |= static_cast<unsigned>(at < lo) << e;
+        here |= static_cast<unsigned>((at >= lo) & ((at < hi) | last_bin) & (v > -INFINITY)) << e;
+        close |= static_cast<unsigned>(v >= weight.near_from) << e;
+      }
+      above += weight.of_some(r, before, close);
+      for (; here; here &= here - 1) {
+        const int e = __ffs(here) - 1;
+        const float v = Weight<DT>::pick(r, e);
+        inside += weigh(v);
+        if (few) list(w.h, v, token + e);
       }
     });
     const Taken got = taken<Add, Add>(w, above, inside);
@@ -726,7 +779,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
   SampleShared& h = *reinterpret_cast<SampleShared*>(smem);
   __shared__ Exchange x;
   __shared__ double table[kTable];
-  const int parts = p.c.parts, rank = blockIdx.x % parts, row = blockIdx.x / parts, tid = threadIdx.x;
+  const int parts = p.c.parts, rank = blockIdx.x & (parts - 1), row = blockIdx.x >> p.c.shift, tid = threadIdx.x;
   if (parts > 1) cluster_barrier_arrive();
   wait_for_inputs();
   RowSlice<DT> s;
@@ -737,7 +790,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
   const float top_p = p.row_p ? p.row_p[row] : p.p, min_p = p.row_min_p ? p.row_min_p[row] : p.min_p;
   const double u = fmin(fmax(static_cast<double>(p.u[row]), 0.0), 1.0);  // (NaN: 0)
   char* const filtered = p.filtered ? p.filtered + static_cast<long long>(row) * p.stride_filtered * Elem<DT>::bytes : nullptr;
-  table[tid] = exp2(static_cast<double>(tid) / kTable);
+  table[tid] = exp2(static_cast<double>(tid) / kTable + Weight<DT>::scale_of(p.c.V));
   clear_bins(h);
   if (tid < 64) h.steps[tid] = 0;
   if (tid == 0) h.listed = 0;
@@ -791,39 +844,18 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
   const u64 everything = place_of(-FLT_MAX, 0x7fffffff);
   u64 last = everything;  // the last place that is kept; nothing at -inf is
   if (by_k || by_p) {
-    // bins of 1/32 of a power of two of the weight where sums of weights are wanted, else of 1/64 of a logit
-    const float per_half = by_p ? fminf(32.0f * weight.c32x2, 1e30f) : 128.0f;
-    const auto bin_at = [&](float v) { return fmaf(-0.5f, v, weight.half) * per_half; };
-    const auto bin_of = [&](float v) { return min(static_cast<int>(bin_at(v)), kBins - 1); };
-    const auto count_in = [&](float v) {
-      if (v > -INFINITY) {
-        const float at = bin_at(v);
-        const int bin = min(static_cast<int>(at), kBins - 1);
-        atomicAdd(&h.count[bin], 1u);
-        if (by_p && bin < kBins - 1) atomicAdd(&h.lo[bin], static_cast<unsigned>((at - static_cast<float>(bin)) * 16.0f));
-      }
-    };
     u64 total = 0;  // what top-p is a part of
-    bool counted = false;
     if (!by_k || k <= kHeadMost) {
       const float from = reached_by(h, groups, {groups.group}, by_k ? k : min(kHeadGuess, p.c.V));
       u64 sum = 0, mass = 0;
-      if (!by_k) {  // (everything is looked at for the total; the histogram is filled on the way, for rows that want it)
+      unsigned unused = 0;
+      if (!by_k) sum = weight.of_all(s, unused);
+      if (own >= from) {
         s.raw([&](int token, const uint4& r) {
-          sum += weight.of_vector(r, token, Everything());
-#pragma unroll
-          for (int e = 0; e < Elem<DT>::E; ++e) {
-            const float v = entry<DT>(r, e);
-            count_in(v);
-            if (v >= from && v > -INFINITY) {
-              mass += weigh(v);
-              list(h, v, token + e);
-            }
-          }
+          const unsigned in = list_from<DT>(h, from, token, r);
+          if (!by_k)
+            for (unsigned e = in; e; e &= e - 1) mass += weigh(Weight<DT>::pick(r, __ffs(e) - 1));
         });
-        counted = true;
-      } else if (own >= from) {
-        s.raw([&](int token, const uint4& r) { list_from<DT>(h, from, token, r); });
       }
       const Taken got = taken<Add, Add>(w, sum, mass);
       total = got.sum;
@@ -866,15 +898,39 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
         return;
       }
     }
-    if (!counted) {
-      s.entries([&](int, float v) { count_in(v); });
-      row_barrier(parts);
+    // Bins of 1/64 of a logit for a top-k alone, of 1/32 of a power of two of the weight for both.  For a top-p alone they reach as far as its limit may lie: all logits
+    // whose weight is below (1 - p) / vocab of the total have less than (1 - p) of it together, and are left out.
+    bool cut = false;
+    float per_unit = 32.0f;
+    if (by_p && !by_k) {
+      const double at = (1.0 - static_cast<double>(fmaxf(top_p, 0.0f))) * static_cast<double>(total) / p.c.V;  // that weight, in units
+      cut = at >= 16.0;                                                                                      // (far from the rounding to units)
+      if (cut) per_unit = static_cast<float>(kBins - 2) / fmaxf(static_cast<float>(weight.scale) - log2f(static_cast<float>(at)) + 0.1f, 0.01f);
     }
+    const float per_half = by_p ? fminf(per_unit * weight.c32x2, 1e30f) : 128.0f;
+    const auto bin_at = [&](float v) { return fmaf(-0.5f, v, weight.half) * per_half; };
+    const auto bin_of = [&](float v) { return min(static_cast<int>(bin_at(v)), kBins - 1); };
+    const bool packed = by_p && p.c.share <= kPackedEntries / Elem<DT>::E;
+    s.raw([&](int, const uint4& r) {
+#pragma unroll
+      for (int e = 0; e < Elem<DT>::E; ++e) {
+        const float v = entry<DT>(r, e);
+        const int eighths = static_cast<int>(bin_at(v) * 8.0f), bin = eighths >> 3;
+        if (v > -INFINITY && (bin < kBins - 1 || !cut)) {
+          const unsigned part = by_p && bin < kBins - 1 ? eighths & 7 : 0;
+          atomicAdd(&h.count[min(bin, kBins - 1)], packed ? 1u << kPackedShift | part : 1u);
+          if (!packed && part) atomicAdd(&h.lo[bin], part);
+        }
+      }
+    });
+    row_barrier(parts);
     Bins b;
-    // the weights of a bin, from the places of its tokens in it (in sixteenths), up to the curvature of exp2 over it (6e-5)
-    merge_bins(w, by_p, false, b, [&](int bin, unsigned count, u64 sixteenths, unsigned) {
-      const float part = static_cast<float>(count) - 0.00133925f * (static_cast<float>(sixteenths) + 0.5f * static_cast<float>(count));  // (1 - 2^(-1/32)) / 16
-      return bin == kBins - 1 ? 0ull : static_cast<u64>(weight.power(-bin * (kTable / 32)) * static_cast<double>(part));
+    // the weights of a bin, from the places of its tokens in it (in eighths), up to the curvature of exp2 over it (1e-4)
+    const float eighth = (1.0f - exp2f(-1.0f / per_unit)) * 0.125f;
+    const double unit = weight.power(0);
+    merge_bins(w, by_p, false, packed, b, [&](int bin, unsigned count, u64 eighths, unsigned) {
+      const float part = static_cast<float>(count) - eighth * (static_cast<float>(eighths) + 0.5f * static_cast<float>(count));
+      return bin == kBins - 1 ? 0ull : static_cast<u64>(unit * static_cast<double>(part * exp2f(static_cast<float>(-bin) / per_unit)));
     });
     if (by_k && static_cast<u64>(k) < b.all_count) {
       const Found f = locate(w, b, false, k);
@@ -900,10 +956,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
   u64 mine = 0;
   unsigned kept = 0;
   if (last == everything && bound == last_logit) {
-    s.raw([&](int token, const uint4& r) {
-      mine += weight.of_vector(r, token, Everything());
-      kept += finite_entries<DT>(r);
-    });
+    mine = weight.of_all(s, kept);
   } else if (own >= bound) {
     s.raw([&](int token, const uint4& r) {
       RunningMax<DT> top;
@@ -975,7 +1028,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_top_kernel(const TopPara
   Shared<kList>& h = *reinterpret_cast<Shared<kList>*>(smem);
   __shared__ Exchange x;
   constexpr int kGroups = kStream ? 2 : 1;  // of a thread
-  const int parts = kStream ? 1 : p.c.parts, rank = kStream ? 0 : blockIdx.x % parts, row = kStream ? blockIdx.x : blockIdx.x / parts, tid = threadIdx.x;
+  const int parts = kStream ? 1 : p.c.parts, rank = kStream ? 0 : blockIdx.x & (parts - 1), row = kStream ? blockIdx.x : blockIdx.x >> p.c.shift, tid = threadIdx.x;
   if (parts > 1) cluster_barrier_arrive();
   wait_for_inputs();
   RowSlice<DT> s;
@@ -983,7 +1036,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_top_kernel(const TopPara
   if (tid < 64) h.steps[tid] = 0;
   if (tid == 0) h.listed = h.hits = 0;
   Row<Shared<kList>> w = {h, x, parts, rank, 0, 0};
-  const float c = fminf(static_cast<float>(1.4426950408889634 / static_cast<double>(p.T)), 3e38f);
+  const float c = p.scale;
   const int half = (p.c.seg / 32 + kGroups - 1) / kGroups * 32;  // vectors of a warp's groups
   Groups groups;
   float own[kGroups], mine;  // the largest of this thread's groups, and of them
@@ -1065,7 +1118,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_top_kernel(const TopPara
     });
     row_barrier(parts);
     Bins b;
-    merge_bins(w, false, false, b, [](int, unsigned, u64, unsigned) { return 0ull; });
+    merge_bins(w, false, false, false, b, [](int, unsigned, u64, unsigned) { return 0ull; });
     u64 from = 0;  // of places
     if (static_cast<u64>(p.k) < b.all_count) {
       const Found f = locate(w, b, false, p.k);
@@ -1143,6 +1196,7 @@ cos_status launch_rows(P& p, int rows, int vocab, int dtype, int device, size_t 
   }
   p.c.V = vocab;
   p.c.parts = plan.parts;
+  p.c.shift = __builtin_ctz(plan.parts);
   p.c.share = plan.share;
   p.c.seg = plan.seg;
   p.c.res = plan.res;
@@ -1229,6 +1283,7 @@ extern "C" cos_status cos_top_logits(const cos_top_args* a, void* cuda_stream) {
   p.c.stride = a->stride_row;
   p.k = a->k;
   p.T = a->temperature;
+  p.scale = fminf(static_cast<float>(1.4426950408889634 / static_cast<double>(a->temperature)), 3e38f);
   p.values = a->values;
   p.ids = a->ids;
   p.lse = a->lse;

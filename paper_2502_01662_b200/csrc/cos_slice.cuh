@@ -151,16 +151,17 @@ struct RowSlice {
   // itself, so no barrier is needed).
   __device__ __forceinline__ void start() const {
     const int last = min(end, res);
-    for (int i = begin + (threadIdx.x & 31); i < last; i += 32) {
-      const int x = token(i);
-      const char* from = base + (static_cast<long long>(v0) + i) * 16;
-      if (x >= 0 && x <= V - E) {
-        const unsigned to = static_cast<unsigned>(__cvta_generic_to_shared(kept + i));
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
-      } else {
-        kept[i] = ragged(from, x);
-      }
+    int i = begin + (threadIdx.x & 31);
+    const int whole = static_cast<int>(min(static_cast<long long>(last), (static_cast<long long>(V) + off) / E - v0));  // vectors before it end inside the row
+    if (i < last && v0 + i == 0 && off != 0) {
+      kept[i] = ragged(base, token(i));
+      i += 32;
     }
+    const char* from = base + (static_cast<long long>(v0) + i) * 16;
+    unsigned to = static_cast<unsigned>(__cvta_generic_to_shared(kept + i));
+#pragma unroll 4
+    for (; i < whole; i += 32, from += 512, to += 512) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+    if (i < last) kept[i] = ragged(from, token(i));  // (the row's last vector: no lane has more than one behind `whole`)
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
   __device__ __forceinline__ void finish() const { asm volatile("cp.async.wait_all;" ::: "memory"); }

@@ -158,17 +158,18 @@ struct NormaliserRoom {
   Normaliser warp[kSliceWarps], block[kSliceParts];
 };
 // ... from the warps' (m the same for the lanes of one, z a lane's).
+template <int kWarps>
 __device__ __forceinline__ Normaliser row_normaliser(NormaliserRoom& room, int parts, int rank, float c, float m, double z) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   z = warp_sum(z);
   if (lane == 0) room.warp[warp] = {m, z};
   __syncthreads();
   if (warp == 0) {
-    const Normaliser a = room.warp[lane & (kSliceWarps - 1)];
+    const Normaliser a = room.warp[lane & (kWarps - 1)];
     m = a.m;
 #pragma unroll
-    for (int d = kSliceWarps / 2; d > 0; d >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, d));
-    z = lane < kSliceWarps && a.m != -INFINITY ? a.z * static_cast<double>(ex2_approx((a.m - m) * c)) : 0.0;
+    for (int d = kWarps / 2; d > 0; d >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, d));
+    z = lane < kWarps && a.m != -INFINITY ? a.z * static_cast<double>(ex2_approx((a.m - m) * c)) : 0.0;
     z = warp_sum(z);
     if (parts == 1) {
       if (lane == 0) room.block[0] = {m, z};
@@ -199,7 +200,7 @@ __device__ __forceinline__ Normaliser normaliser(NormaliserRoom& room, const Row
     const f32x2 minus_m = pack2(-m, -m), cc = pack2(c, c);
     s.raw([&](int, const uint4& r) { z += static_cast<double>(sum_exp2<DT>(r, minus_m, cc)); });
   }
-  return row_normaliser(room, parts, rank, c, m, z);
+  return row_normaliser<kSliceWarps>(room, parts, rank, c, m, z);
 }
 
 // q(x) times the scale, from the statistics of the student.
@@ -289,8 +290,8 @@ __device__ __forceinline__ void finish_loss(const DistillParams& p, int row, con
 }
 
 // The loss where there are rows enough for a block each: a row goes by in registers, against a running maximum of each lane.
-template <int DT>
-__global__ void __launch_bounds__(kSliceThreads, 2) cos_distill_stream_kernel(const DistillParams p) {
+template <int DT, int kWarps>
+__global__ void __launch_bounds__(32 * kWarps, 32 / kWarps) cos_distill_stream_kernel(const DistillParams p) {
   __shared__ NormaliserRoom room;
   const int row = blockIdx.x;
   RowSlice<DT> s;
@@ -325,7 +326,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_distill_stream_kernel(co
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, d));
   sum.to(m, c);
-  const Normaliser n = row_normaliser(room, 1, 0, c, m, sum.z);
+  const Normaliser n = row_normaliser<kWarps>(room, 1, 0, c, m, sum.z);
   if (threadIdx.x == 0) finish_loss(p, row, st, n, true);
 }
 
@@ -445,8 +446,12 @@ cos_status distill(const cos_distill_args* a, void* cuda_stream) {
   p.share = plan.share;
   p.seg = plan.seg;
   p.res = plan.res;
-  p.early = 2 * plan.sms;
-  if (MODE == kLoss && a->rows >= plan.sms) plan_row(a->vocab, a->dtype, &p.share, &p.seg);
+  p.early = 2 * plan.sms;  // (the first ones to find a place)
+  // The loss takes a block for each row, but for few rows that are long (64 rows of 128256 bf16 9.0 us, on clusters 13.9; 256 rows 15 and 28; 16 rows of 256000 14.1 and 10.9, 64 rows 14.4
+  // and 19.4), of 8 warps where rows are short (256 rows of 32000 bf16 7.5 us, of 16 warps 8.5; 512 rows of 128256 31.1 and 29.3).
+  const long long row_bytes = static_cast<long long>(a->vocab) * bytes;
+  const int stream_warps = MODE != kLoss || (row_bytes > 384 * 1024 && a->rows <= 32) ? 0 : (row_bytes < 96 * 1024 ? 8 : 16);
+  if (stream_warps) plan_row(a->vocab, a->dtype, stream_warps, &p.share, &p.seg);
   p.lists = a->lists;
   p.k = a->k;
   p.ids = a->ids;
@@ -468,7 +473,8 @@ cos_status distill(const cos_distill_args* a, void* cuda_stream) {
       const cudaError_t first = slice_launch(cos_distill_shares_kernel<DT>, p, a->rows, 1, static_cast<size_t>(a->lists) * a->k * (sizeof(double) + sizeof(int) + sizeof(float)), stream, kShareThreads);
       if (first != cudaSuccess) return first;
     }
-    if (MODE == kLoss && a->rows >= plan.sms) return slice_launch(cos_distill_stream_kernel<DT>, p, a->rows, 1, 0, stream);
+    if (stream_warps == 8) return slice_launch(cos_distill_stream_kernel<DT, 8>, p, a->rows, 1, 0, stream, 256);
+    if (stream_warps == 16) return slice_launch(cos_distill_stream_kernel<DT, 16>, p, a->rows, 1, 0, stream, 512);
     return slice_launch(cos_distill_kernel<DT, MODE>, p, a->rows * plan.parts, MODE == kGrad ? 1 : plan.parts, plan.smem, stream);
   };
   e = a->dtype == COS_DTYPE_F32    ? launches(std::integral_constant<int, COS_DTYPE_F32>())

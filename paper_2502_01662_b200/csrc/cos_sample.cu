@@ -26,6 +26,7 @@ constexpr int kBins = 1024, kBinBits = 10, kCandidates = 512, kTopCandidates = C
 // the largest k that a list of that size is used for
 template <int kList>
 constexpr int kMost = kList == kTopCandidates ? COS_TOP_MAX : 288;
+constexpr int kMostKept = 64 * 1024;  // bytes of a slice: two blocks of a multiprocessor have room for that beside what they share
 // A block of so few entries counts those of a bin, and adds up their places in it (in eighths), in one word.
 constexpr int kPackedEntries = 16384, kPackedShift = 17;
 constexpr int kFew = 128;
@@ -1185,14 +1186,14 @@ cos_status launch_rows(P& p, int rows, int vocab, int dtype, int device, size_t 
   OnDevice on(device);
   if (on.error != cudaSuccess) return call_failed("cudaSetDevice", on.error);
   SlicePlan plan;
-  cudaError_t e = slice_plan(device, rows, vocab, dtype, 64 * 1024, true, &plan);
+  cudaError_t e = slice_plan(device, rows, vocab, dtype, kMostKept, true, &plan);
   if (e != cudaSuccess) return call_failed("device query", e);
   if (static_cast<long long>(rows) * plan.parts > 0x7fffffffll) return call_failed(COS_ERR_UNSUPPORTED, "too many rows for one launch");
   if (whole) {  // a block for each row, which stays in memory
     plan.parts = 1;
     plan.res = 0;
     plan.smem = 0;
-    plan_row(vocab, dtype, &plan.share, &plan.seg);
+    plan_row(vocab, dtype, kSliceWarps, &plan.share, &plan.seg);
   }
   p.c.V = vocab;
   p.c.parts = plan.parts;
@@ -1294,10 +1295,10 @@ extern "C" cos_status cos_top_logits(const cos_top_args* a, void* cuda_stream) {
       return dt == COS_DTYPE_F32 ? cos_top_kernel<COS_DTYPE_F32, kList, kStream> : (dt == COS_DTYPE_BF16 ? cos_top_kernel<COS_DTYPE_BF16, kList, kStream> : cos_top_kernel<COS_DTYPE_F16, kList, kStream>);
     });
   };
-  int sms = 0;
-  const cudaError_t e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, a->device);
-  if (e != cudaSuccess) return call_failed("device query", e);
   using Few = std::integral_constant<int, kCandidates>;
   if (a->k > kMost<kCandidates>) return call(std::integral_constant<int, kTopCandidates>(), std::false_type());
-  return a->rows >= sms ? call(Few(), std::true_type()) : call(Few(), std::false_type());
+  // A block for each row where there are rows enough and one does not fit into a block's shared memory (top 64 of 64 rows of 128256 bf16 13.0 us, on clusters 14.0; of 256 19.9 and 47;
+  // of 32 12.7 and 10.2; of 256 rows of 8000 12.7 and 7.3).
+  const bool long_rows = static_cast<long long>(a->vocab) * (a->dtype == COS_DTYPE_F32 ? 4 : 2) > kMostKept;
+  return a->rows >= 48 && long_rows ? call(Few(), std::true_type()) : call(Few(), std::false_type());
 }

@@ -367,10 +367,10 @@ struct SlicePlan {
   size_t smem;
 };
 // (a whole row for one block)
-inline void plan_row(int vocab, int dtype, int* share, int* seg) {
+inline void plan_row(int vocab, int dtype, int warps, int* share, int* seg) {
   const int E = dtype == COS_DTYPE_F32 ? 4 : 8;
   *share = static_cast<int>((static_cast<long long>(vocab) + 2 * (E - 1)) / E);
-  *seg = (*share + 32 * kSliceWarps - 1) / (32 * kSliceWarps) * 32;
+  *seg = (*share + 32 * warps - 1) / (32 * warps) * 32;
 }
 cudaError_t slice_plan(int device, int rows, int vocab, int dtype, int most, bool cluster, SlicePlan* plan);
 

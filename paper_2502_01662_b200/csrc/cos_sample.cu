@@ -108,14 +108,9 @@ struct Weight {
   double m64, c;        // the logit, log2(e) / T
   const double* table;  // 2^(j / 512) in units
   int scale;
-  // A finite float widened (0 and subnormal numbers to next to nothing): integer instructions, of which there are eight times as many a clock as conversions.
-  static __device__ __forceinline__ double widen(float v) {
-    const unsigned u = __float_as_uint(v);
-    return __hiloint2double(static_cast<int>((((u & 0x7fffffffu) >> 3) + 0x38000000u) | (u & 0x80000000u)), DT == COS_DTYPE_F32 ? static_cast<int>(u << 29) : 0);
-  }
   __device__ __forceinline__ void init(float m, float T, int V, const double* table_) {
     half = 0.5f * m;
-    m64 = widen(m);
+    m64 = static_cast<double>(m);
     c = 1.4426950408889634 / static_cast<double>(T);
     c32x2 = fmaxf(fminf(static_cast<float>(2.0 * c), 3e38f), 1e-37f);  // (-inf is infinitely far at any temperature)
     near_from = fmaxf(static_cast<float>(m64 - kNear / c), -FLT_MAX);
@@ -131,7 +126,7 @@ struct Weight {
   // Not rounded to the unit; l is at most 2^40 units of the temperature below the largest.
   __device__ __forceinline__ double exact(float l) const {
     constexpr double kRound = 13194139533312.0;  // 1.5 * 2^43: sums with it are multiples of 2^-9
-    const double d = widen(l) - m64;
+    const double d = static_cast<double>(l) - m64;
     const double k = fma(d, c, kRound);
     const double r = fma(d, c, kRound - k);
     const int n = __double2loint(k);
@@ -199,9 +194,9 @@ struct Weight {
     for (unsigned e = kept & ~close; e; e &= e - 1) sum += far(pick(r, __ffs(e) - 1));
     return sum;
   }
-  // Sum over all entries of this lane.  Those far below the largest go by 32 bits, all at once (near ones among them, modulo 2^32, and are taken off again); the near ones
-  // by 64-bit instructions in a second pass, in which every lane goes from one of its vectors with any to the next: few where the tail is long, and half the
-  // time of the sweep where most entries are near.
+  // Sum over all entries of this lane.  Vectors far below the largest go by 32 bits; those with near entries in a second pass, in which every lane goes from one of its own to
+  // the next (few where the tail is long): the near ones by 64-bit instructions, the others by 32 bits with all of the vector, modulo 2^32, from which what that makes
+  // of the near ones is taken off again.
   __device__ __forceinline__ u64 of_all(const RowSlice<DT>& s, unsigned& finite) const {
     const int first = s.begin + (threadIdx.x & 31);
     u64 sum = 0;
@@ -214,9 +209,10 @@ struct Weight {
         const uint4 r = s.at(i);
         RunningMax<DT> top;
         top.add(r);
-        tail += far_vector(r);
         finite += finite_entries<DT>(r);
-        any |= static_cast<unsigned>(top.value() >= near_from) << bit;
+        const bool close = top.value() >= near_from;
+        if (!close) tail += far_vector(r);
+        any |= static_cast<unsigned>(close) << bit;
       }
       for (; any; any &= any - 1) {
         const uint4 r = s.at(block + 32 * (__ffs(any) - 1));
@@ -228,11 +224,10 @@ struct Weight {
 #pragma unroll
           for (int e = 0; e < Elem<DT>::E; ++e) bits += near_bits(entry<DT>(r, e));
           sum += bits - Elem<DT>::E * kUnits;
-          as_far = far_vector(r);
         } else {
           sum += near_ones(r, head, as_far);
+          tail += far_vector(r) - as_far;
         }
-        tail -= as_far;
       }
     }
     return sum + tail;

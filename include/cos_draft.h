@@ -63,8 +63,9 @@ typedef struct {
  *           kept (so the first one always is);
  *   min-p   of these, a token is kept where w(x) >= min_p.
  * The draw is the inverse of the cumulative sum in order of the index: the lowest kept x with sum_{y <= x} w(y) >= u * S.
- * Weights are evaluated in 64 bits and summed as whole multiples of 2^-(63 - ceil(log2 vocab)) (2^-46 at most) of the largest
- * one, so sums do not depend on any order: two calls on the same inputs agree bit by bit.
+ * Weights are evaluated in 64 bits (those below 2^-36 of the largest one in 32, to 2^-17 of themselves) and summed as whole
+ * multiples of 2^-(63 - ceil(log2 vocab)) (2^-46 at the least) of the largest one, so sums do not depend on any order: two calls
+ * on the same inputs agree bit by bit.
  */
 cos_status cos_sample(const cos_sample_args* args, void* cuda_stream);
 
@@ -119,7 +120,7 @@ typedef struct {
  *   loss = sum_x t(x) (ln t(x) - ln q(x)),   gradient = row_weight / T * (P q(x) - t(x)),  P = sum_x t(x).
  * +inf where a token with a share has the logit -inf.  A row without a share (padding) has loss 0 and gradient 0 and is not read.
  *   cos_distill_loss  loss and statistics (row_weights, grad are not looked at)
- *   cos_distill_grad  the gradient, from the statistics of the same student, lists and T (loss, values and lse are not looked at)
+ *   cos_distill_grad  the gradient, from the statistics of the same student, lists and T (loss is not looked at)
  *   cos_distill_step  loss and gradient, reading the student once
  */
 cos_status cos_distill_loss(const cos_distill_args* args, void* cuda_stream);

@@ -96,6 +96,11 @@ def _small(t, name: str, shape, dtype, device) -> int:
     return t.data_ptr()
 
 
+def _written(torch, t):
+    """A tensor of the caller's that the library writes: autograd is told, as by an operation in place."""
+    torch.autograd.graph.increment_version(t)
+
+
 def _stream_of(torch, device, stream, made):
     """The address of the stream of a call; tensors made for a stream that is not the current one stay with it."""
     if stream is None:
@@ -149,6 +154,8 @@ def sample(logits, uniforms, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, fil
         out["filtered"] = filtered
     lib = _library()
     _check(lib, lib.cos_sample(ctypes.byref(a), _stream_of(torch, device, stream, made)))
+    if filtered is not False:
+        _written(torch, filtered)
     return out
 
 
@@ -298,4 +305,5 @@ def distill_step(student, ids, values, row_weights, lse=None, weights: Optional[
     a.loss, a.statistics, a.grad = loss.data_ptr(), statistics.data_ptr(), grad.data_ptr()
     lib = _library()
     _check(lib, lib.cos_distill_step(ctypes.byref(a), _stream_of(torch, device, stream, made)))
+    _written(torch, grad)
     return {"loss": loss, "grad": grad}

@@ -13,6 +13,10 @@ The verification call is passed in (`verify`): the product path hands in `gpu_ve
 the CUDA library; this module holds no verification arithmetic of its own.  The models are stand-ins:
 `TableModel` maps a context (last token, position) to a row of a seeded logit table, so that every
 call is reproducible on any machine.
+
+A proposal is drawn from the proposer's softmax, or, where a proposer is passed in (`propose`: `GpuProposer`, or anything with
+its methods), from what top-k, top-p and min-p leave of it.  Every model's distribution is then that one wherever it
+is used: as q, in the combination, and for a bonus token.
 """
 from __future__ import annotations
 
@@ -81,7 +85,7 @@ class AlternateProposal:
     """Algorithm 1.  models = (M_q, M_p): M_q is the default proposer; gammas = (gamma_q, gamma_p)."""
 
     def __init__(self, models: Sequence[TableModel], gammas: Sequence[int], temperature: float, verify: VerifyFn,
-                 propose_seed: int = 1, verify_seed: int = 2, keep_history: bool = False):
+                 propose_seed: int = 1, verify_seed: int = 2, keep_history: bool = False, propose=None):
         if len(models) != 2 or len(gammas) != 2 or min(gammas) < 1:
             raise ValueError("two models and two proposal lengths >= 1")
         if models[0].vocab != models[1].vocab:
@@ -91,11 +95,14 @@ class AlternateProposal:
         self.verify_seed = verify_seed
         self._u = np.random.Generator(np.random.Philox(key=propose_seed))
         self.keep_history = keep_history
+        self.propose = _checked(propose, self.T)
 
     # Propose: one token from model i after `prefix`, at the temperature of the run
     def _propose_one(self, i: int, prefix: Sequence[int]) -> int:
         m = self.models[i]
         m.calls += 1
+        if self.propose is not None:
+            return self.propose.draw(m.logits(prefix), self._u.random())
         l = m.logits(prefix).astype(np.float64)
         if self.T == 0.0:
             return int(np.argmax(l))
@@ -130,6 +137,7 @@ class AlternateProposal:
                 ctx = S + T[:j]
                 logits[0, 0, j] = self.models[0].logits(ctx)
                 logits[1, 0, j] = self.models[1].logits(ctx)
+            logits = _laws(self.propose, logits)
             drafts = np.asarray(T, dtype=np.int32).reshape(1, g)
             a, out, prob = self.verify(logits, drafts, proposer, verifier, self.verify_seed, st.cycles)
             emitted = [int(x) for x in out[: a + 1]] if a < g else [int(x) for x in out[:g]]
@@ -168,7 +176,7 @@ class CollaborativeSpeculation:
     Sec. 3.3 and of the walk-through in App. B; the listing would let the scoring model propose first)."""
 
     def __init__(self, models: Sequence[TableModel], gammas: Sequence[int], temperature: float, verify: VerifyFn,
-                 propose_seed: int = 1, verify_seed: int = 2, keep_events: bool = False):
+                 propose_seed: int = 1, verify_seed: int = 2, keep_events: bool = False, propose=None):
         if len(models) < 2 or len(models) != len(gammas) or min(gammas) < 1:
             raise ValueError("n >= 2 models and one proposal length >= 1 for each")
         self.models, self.gammas, self.T = list(models), list(gammas), float(temperature)
@@ -178,6 +186,7 @@ class CollaborativeSpeculation:
         self.keep_events = keep_events
         self.events: List[Event] = []
         self.calls = 0         # verification calls so far: the counter offset of the next one
+        self.propose = _checked(propose, self.T)
 
     def _log(self, *a):
         if self.keep_events:
@@ -186,6 +195,8 @@ class CollaborativeSpeculation:
     def _sample(self, i: int, prefix: Sequence[int]) -> int:
         m = self.models[i]
         m.calls += 1
+        if self.propose is not None:
+            return self.propose.draw(m.logits(prefix), self._u.random())
         l = m.logits(prefix).astype(np.float64)
         if self.T == 0.0:
             return int(np.argmax(l))
@@ -221,7 +232,7 @@ class CollaborativeSpeculation:
             self.models[i].calls += 1
             st.scored += 1
             self._log("score", i, len(Sc))
-            row = self.models[i].logits(S + Sc)
+            row = _laws(self.propose, self.models[i].logits(S + Sc))
             lg = np.broadcast_to(row, (n, 1, 1, V)).astype(np.float32).copy()
             _, out, prob = self.verify(lg, np.zeros((1, 0), np.int32), 0, i, self.verify_seed, self.calls)
             self.calls += 1
@@ -237,6 +248,7 @@ class CollaborativeSpeculation:
                     ctx = S + Sc[:j]
                     for k in range(n):
                         lg[k, 0, j] = self.models[k].logits(ctx)
+                lg = _laws(self.propose, lg)
                 table = np.asarray(owner[:L] + [0], dtype=np.int32).reshape(1, L + 1)
                 a, out, _ = self.verify(lg, np.asarray(Sc[:L], np.int32).reshape(1, L), table, -1, self.verify_seed,
                                         self.calls)
@@ -258,6 +270,43 @@ class CollaborativeSpeculation:
                 propose(i, self.gammas[i] - 1)            # the bonus token was the first of model i's proposal
         st.tokens = len(S) - start
         return S[start:], st
+
+
+def _checked(propose, temperature: float):
+    if propose is not None and propose.temperature != temperature:
+        raise ValueError("the proposer's temperature is not the run's")
+    return propose
+
+
+def _laws(propose, logits: np.ndarray) -> np.ndarray:
+    return logits if propose is None else propose.law(logits)
+
+
+class GpuProposer:
+    """Proposals drawn by the CUDA library (cos_sample) for the schedulers, from host rows of logits: the temperature of the run
+    and top-k, top-p and min-p (0, 1 and 0: no limit).
+
+    `draw` gives a token of one row; `law` the rows with -inf at every token that could not have been drawn, which
+    is what the verification has to take as the models' logits.  (Ruled-out tokens have a meaning in an ensemble; a
+    logit-linear combination of -inf is not a number, and such a run takes no limits.)"""
+
+    def __init__(self, temperature: float, top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0, device: int = 0):
+        self.temperature = float(temperature)
+        self._limits = (self.temperature, int(top_k), float(top_p), float(min_p))
+        self._device = f"cuda:{device}"
+
+    def _sample(self, rows: np.ndarray, uniforms: np.ndarray, filtered: bool) -> dict:
+        import torch
+        from .draft import sample
+        logits = torch.from_numpy(np.ascontiguousarray(rows, dtype=np.float32)).to(self._device)
+        return sample(logits, torch.from_numpy(uniforms.astype(np.float32)).to(self._device), *self._limits, filtered=filtered)
+
+    def draw(self, row: np.ndarray, uniform: float) -> int:
+        return int(self._sample(row.reshape(1, -1), np.array([uniform]), False)["tokens"][0])
+
+    def law(self, rows: np.ndarray) -> np.ndarray:
+        flat = rows.reshape(-1, rows.shape[-1])
+        return self._sample(flat, np.zeros(flat.shape[0]), True)["filtered"].cpu().numpy().reshape(rows.shape)
 
 
 def gpu_verify(combine: int, weights: Sequence[float], temperature: float, vocab: int, mask_model: int = -1,

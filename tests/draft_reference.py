@@ -1,8 +1,8 @@
 """The proposer's operators in 64 bits (numpy), row by row from their definitions, and the tolerances they are held to.
 
 Sampling.  The library sums weights as whole multiples of a unit of 2^-scale of the largest one, scale = min(46, 63 - ceil(log2 V)); each is off by half a
-unit and by the error of its 64-bit evaluation (below 2^-44 of it), so no sum is off by more than `slack` = V (unit / 2) + S 2^-43, in units of the largest
-weight.  `check_sample` wants every border (of top-p, of the draw) on the right side of its threshold up to that, and everything else exact."""
+unit and by the error of its evaluation (below 2^-44 of it; weights below 2^-36 by 2^-17 of them, at most 2^-53), so no sum is off by more than
+`slack` = V (unit / 2 + 2^-53) + S 2^-43, in units of the largest weight.  `check_sample` wants every border (of top-p, of the draw) on the right side of its threshold up to that, and everything else exact."""
 import math
 
 import numpy as np
@@ -29,7 +29,7 @@ def check_sample(x, u, T, k, p, least, token, prob, kept, status, law=None):
     else:
         with np.errstate(under="ignore"):
             w = np.exp((x[line] - x[line[0]]) / T)
-        slack = V * 2.0 ** -(min(46, 63 - math.ceil(math.log2(V))) + 1) + w.sum() * 2.0 ** -43
+        slack = V * (2.0 ** -(min(46, 63 - math.ceil(math.log2(V))) + 1) + 2.0 ** -53) + w.sum() * 2.0 ** -43
         n = line.size if k <= 0 else min(k, line.size)
         if p < 1.0:
             before = np.concatenate(([0.0], np.cumsum(w[:n])))

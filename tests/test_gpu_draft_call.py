@@ -73,6 +73,16 @@ def test_a_student_changed_in_place_is_noticed(monkeypatch):
     both(monkeypatch, change)
 
 
+def test_what_the_library_writes_in_place_is_noticed():
+    ids, values, rw = torch.zeros((3, 2), dtype=torch.int32, device="cuda"), torch.zeros((3, 2), device="cuda"), torch.ones(3, device="cuda")
+    for write in (lambda t: pkg.sample(t, rw * 0.5, top_k=3, filtered=t), lambda t: pkg.distill_step(t, ids, values, rw, grad=t)):
+        mid = torch.randn((3, 100), device="cuda", requires_grad=True) * 1.0
+        loss = pkg.distill_loss(mid, ids, values)
+        write(mid.detach())
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.sum().backward()
+
+
 def test_only_once_differentiable(monkeypatch):
     s = torch.randn((3, 100), device="cuda", requires_grad=True)
     ids, values = torch.zeros((3, 2), dtype=torch.int32, device="cuda"), torch.zeros((3, 2), device="cuda")

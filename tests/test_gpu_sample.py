@@ -163,6 +163,13 @@ def test_rows_longer_than_shared_memory(dtype):
     assert torch.equal(x, want["filtered"])
 
 
+def test_a_row_of_millions():
+    """More vectors of a lane than fit into a word of bits."""
+    x, u = make(1, 5_000_011, "bf16", seed=14, sigma=4.0)
+    for k, p in ((0, 1.0), (0, 0.7), (2000, 0.9)):
+        run(x, u, 1.0, k, p)
+
+
 def test_offsets_past_32_bits():
     V, stride = 1000, (1 << 31) + 24
     buf = torch.empty(2 * stride + V, dtype=torch.bfloat16, device="cuda")

@@ -76,7 +76,7 @@ typedef struct {
   int32_t dtype;
   int32_t device;
   int32_t k;          /* 1 .. min(COS_TOP_MAX, vocab)                                                   */
-  float temperature;  /* T > 0: of the log-sum-exp only                                                 */
+  double temperature; /* T > 0: of the log-sum-exp only                                                 */
   float* values;      /* out [rows][k]: the k largest logits, the largest first, the lowest index first */
                       /* among equals; -inf where the row has fewer tokens                              */
   int32_t* ids;       /* out [rows][k]: their tokens, -1 where there is none                            */
@@ -103,7 +103,7 @@ typedef struct {
                           /* vocabulary: shares are the teacher's probabilities, what is not listed is  */
                           /* left out.  NULL: shares are the softmax over the list                      */
   float weights[COS_MAX_MODELS]; /* >= 0, of the lists (Eq. 4)                                          */
-  float temperature;      /* T > 0, of teachers and student                                             */
+  double temperature;     /* T > 0, of teachers and student                                             */
   const float* row_weights; /* [rows]: what the loss of each row counts in the sum whose gradient is    */
                           /* wanted; rows of weight 0 have gradient 0 whatever they hold                */
   float* loss;            /* out [rows] */

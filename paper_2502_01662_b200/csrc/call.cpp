@@ -211,6 +211,10 @@ bool of_rows(PyObject* o, const at::Tensor& like, int64_t rows, at::ScalarType t
   *one = static_cast<T>(v);
   return true;
 }
+bool number(PyObject* o, double* v) {
+  const double* each = nullptr;
+  return !THPVariable_Check(o) && of_rows(o, at::Tensor(), 0, at::kDouble, v, &each);
+}
 PyObject* dict_of(std::initializer_list<std::pair<const char*, at::Tensor>> items) {
   PyObject* d = PyDict_New();
   for (const auto& item : items) {
@@ -284,10 +288,9 @@ PyObject* top_logits(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   {
     const at::Tensor* logits = nullptr;
     cos_top_args v = {};
-    const float* none = nullptr;
     const int32_t* no_k = nullptr;
-    if (!rows_of(a[1], &logits, &v.stride_row, &v.dtype) || THPVariable_Check(a[2]) || THPVariable_Check(a[3])) Py_RETURN_NONE;
-    if (!of_rows(a[2], *logits, 0, at::kInt, &v.k, &no_k) || !of_rows(a[3], *logits, 0, at::kFloat, &v.temperature, &none)) Py_RETURN_NONE;
+    if (!rows_of(a[1], &logits, &v.stride_row, &v.dtype) || THPVariable_Check(a[2])) Py_RETURN_NONE;
+    if (!of_rows(a[2], *logits, 0, at::kInt, &v.k, &no_k) || !number(a[3], &v.temperature)) Py_RETURN_NONE;
     const int64_t rows = logits->size(0), vocab = logits->size(1), k = v.k;
     if (k < 1 || k > COS_TOP_MAX || k > vocab) Py_RETURN_NONE;
     const auto options = logits->options().requires_grad(false);
@@ -334,8 +337,7 @@ bool distill_of(PyObject* const* a, cos_distill_args* v, const at::Tensor** stud
       if (THPVariable_Check(w) || !of_rows(w, s, 0, at::kFloat, &v->weights[i], &none)) return false;
     }
   }
-  const float* none = nullptr;
-  if (THPVariable_Check(a[5]) || !of_rows(a[5], s, 0, at::kFloat, &v->temperature, &none)) return false;
+  if (!number(a[5], &v->temperature)) return false;
   v->student = s.data_ptr();
   v->rows = static_cast<int32_t>(rows);
   v->vocab = static_cast<int32_t>(s.size(1));
@@ -381,7 +383,7 @@ struct DistillLoss : torch::autograd::Function<DistillLoss> {
       v.stride_student = v.rows > 1 ? student.stride(0) : v.vocab;
       v.dtype = student.scalar_type() == at::kFloat ? COS_DTYPE_F32 : (student.scalar_type() == at::kBFloat16 ? COS_DTYPE_BF16 : COS_DTYPE_F16);
       v.device = student.get_device();
-      v.temperature = static_cast<float>(numbers[0]);
+      v.temperature = numbers[0];
       v.lists = static_cast<int32_t>(numbers[1]);
       v.k = static_cast<int32_t>(numbers[2]);
       for (int i = 0; i < v.lists; ++i) v.weights[i] = static_cast<float>(numbers[3 + i]);

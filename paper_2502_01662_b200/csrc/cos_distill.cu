@@ -33,8 +33,10 @@ struct DistillParams {
   const float* values;
   const float* lse;
   float w[COS_MAX_MODELS];
-  float T, c;    // c = log2(e) / T
+  float c;       // log2(e) / T
   double inv_T;
+  double inv_c;  // 1 / T as `c` has it: the student's listed logits go by the temperature of its normaliser, or the rounding of c (3e-8) comes in times the distance
+                 // of the likely logits from the largest one (15 and more) instead of from the listed ones
   const float* row_weights;
   float* loss;
   float* statistics;
@@ -255,7 +257,7 @@ __global__ void __launch_bounds__(kShareThreads) cos_distill_shares_kernel(const
   int at = 0;
   while (at < n && !(sh.t[at] != 0.0 && sh.id[at] < p.V)) ++at;
   const float ref = at < n ? sh.s[at] : 0.0f;
-  const double base = fabsf(ref) < INFINITY ? static_cast<double>(ref) : 0.0, inv_T = p.inv_T;
+  const double base = fabsf(ref) < INFINITY ? static_cast<double>(ref) : 0.0;
   float* const shares = shares_of(p, row);
   double listed = 0.0;
   for (int e = threadIdx.x; e < n; e += kShareThreads) {
@@ -270,7 +272,7 @@ __global__ void __launch_bounds__(kShareThreads) cos_distill_shares_kernel(const
           t += sh.t[j];
         }
       if (!first) t = 0.0;
-      if (t != 0.0) listed += t * (log(t) - (static_cast<double>(sh.s[e]) - base) * inv_T);
+      if (t != 0.0) listed += t * (log(t) - (static_cast<double>(sh.s[e]) - base) * p.inv_c);
     }
     shares[e] = static_cast<float>(t);
   }
@@ -280,9 +282,8 @@ __global__ void __launch_bounds__(kShareThreads) cos_distill_shares_kernel(const
 
 __device__ __forceinline__ float log2_of(const Normaliser& z) { return z.m == -INFINITY ? __int_as_float(0x7fc00000) : log2f(static_cast<float>(z.z)); }
 __device__ __forceinline__ void finish_loss(const DistillParams& p, int row, const Statistics& st, const Normaliser& z, bool keep) {
-  const double inv_T = p.inv_T;
   const float log_z = log2_of(z);
-  p.loss[row] = z.m == -INFINITY ? log_z : static_cast<float>(st.listed + st.mass64 * ((static_cast<double>(z.m) - static_cast<double>(st.reference)) * inv_T + log(z.z)));
+  p.loss[row] = z.m == -INFINITY ? log_z : static_cast<float>(st.listed + st.mass64 * ((static_cast<double>(z.m) - static_cast<double>(st.reference)) * p.inv_c + log(z.z)));
   if (keep) {
     statistics_of(p, row)->m = z.m;
     statistics_of(p, row)->log_z = log_z;
@@ -415,7 +416,7 @@ cos_status distill(const cos_distill_args* a, void* cuda_stream) {
     return call_failed(COS_ERR_INVALID_ARG, "lists must be in [1, COS_MAX_MODELS] and lists * k in [1, COS_TOP_MAX]");
   for (int g = 0; g < a->lists; ++g)
     if (!(a->weights[g] >= 0.0f && a->weights[g] < INFINITY)) return call_failed(COS_ERR_INVALID_ARG, "weights must be finite and >= 0");
-  if (!(a->temperature > 0.0f && a->temperature < INFINITY)) return call_failed(COS_ERR_INVALID_ARG, "temperature must be finite and > 0");
+  if (!(a->temperature > 1e-300 && a->temperature < 1e300)) return call_failed(COS_ERR_INVALID_ARG, "temperature must be finite and > 0 (1e-300 to 1e300)");
   const int bytes = a->dtype == COS_DTYPE_F32 ? 4 : 2;
   if (misaligned(a->student, bytes)) return call_failed(COS_ERR_ALIGNMENT, "student pointer not aligned to its element type");
   if (MODE != kGrad && !a->loss) return call_failed(COS_ERR_INVALID_ARG, "null device pointer");
@@ -458,9 +459,9 @@ cos_status distill(const cos_distill_args* a, void* cuda_stream) {
   p.values = a->values;
   p.lse = a->lse;
   for (int g = 0; g < a->lists; ++g) p.w[g] = a->weights[g];
-  p.T = a->temperature;
-  p.c = fminf(static_cast<float>(1.4426950408889634 / static_cast<double>(p.T)), 3e38f);
-  p.inv_T = 1.0 / static_cast<double>(p.T);
+  p.c = static_cast<float>(fmin(1.4426950408889634 / a->temperature, 3e38));
+  p.inv_T = 1.0 / a->temperature;
+  p.inv_c = p.c < 3e38f ? static_cast<double>(p.c) * 0.6931471805599453 : p.inv_T;
   p.row_weights = a->row_weights;
   p.loss = a->loss;
   p.statistics = a->statistics;

@@ -57,7 +57,8 @@ struct SampleParams {
 struct TopParams {
   Common c;
   int k;
-  float T, scale;  // scale = log2(e) / T
+  double inv_T;
+  float scale;  // log2(e) / T
   float* values;
   int* ids;
   float* lse;
@@ -1104,7 +1105,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_top_kernel(const TopPara
   } else {
     sum = double_of(exchange<AddDouble>(x, w.turn, parts, rank, bits_of(sum)).a);
   }
-  if (rank == 0 && tid == 0) p.lse[row] = static_cast<float>(static_cast<double>(m) / static_cast<double>(p.T) + log(sum));
+  if (rank == 0 && tid == 0) p.lse[row] = static_cast<float>(static_cast<double>(m) * p.inv_T + log(sum));
   if (n > kList) {
     const auto bin_of = [&](float v) { return min(static_cast<int>(fmaf(-0.5f, v, 0.5f * m) * 128.0f), kBins - 1); };
     clear_bins(h);
@@ -1273,13 +1274,13 @@ extern "C" cos_status cos_top_logits(const cos_top_args* a, void* cuda_stream) {
   if (!a->values || !a->ids || !a->lse) return call_failed(COS_ERR_INVALID_ARG, "null device pointer");
   if (misaligned4(a->values) || misaligned4(a->ids) || misaligned4(a->lse)) return call_failed(COS_ERR_ALIGNMENT, "an int32/float pointer is not 4-byte aligned");
   if (a->k < 1 || a->k > COS_TOP_MAX || a->k > a->vocab) return call_failed(COS_ERR_INVALID_ARG, "k must be in [1, min(COS_TOP_MAX, vocab)]");
-  if (!(a->temperature > 0.0f)) return call_failed(COS_ERR_INVALID_ARG, "temperature must be > 0");
+  if (!(a->temperature > 1e-300 && a->temperature < 1e300)) return call_failed(COS_ERR_INVALID_ARG, "temperature must be finite and > 0 (1e-300 to 1e300)");
   TopParams p = {};
   p.c.logits = a->logits;
   p.c.stride = a->stride_row;
   p.k = a->k;
-  p.T = a->temperature;
-  p.scale = fminf(static_cast<float>(1.4426950408889634 / static_cast<double>(a->temperature)), 3e38f);
+  p.inv_T = 1.0 / a->temperature;
+  p.scale = static_cast<float>(fmin(1.4426950408889634 / a->temperature, 3e38));
   p.values = a->values;
   p.ids = a->ids;
   p.lse = a->lse;

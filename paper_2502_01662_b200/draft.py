@@ -30,7 +30,7 @@ class cos_sample_args(ctypes.Structure):
 class cos_top_args(ctypes.Structure):
     _fields_ = [
         ("logits", ctypes.c_void_p), ("stride_row", ctypes.c_int64), ("rows", ctypes.c_int32), ("vocab", ctypes.c_int32),
-        ("dtype", ctypes.c_int32), ("device", ctypes.c_int32), ("k", ctypes.c_int32), ("temperature", ctypes.c_float),
+        ("dtype", ctypes.c_int32), ("device", ctypes.c_int32), ("k", ctypes.c_int32), ("temperature", ctypes.c_double),
         ("values", ctypes.c_void_p), ("ids", ctypes.c_void_p), ("lse", ctypes.c_void_p),
     ]
 
@@ -40,7 +40,7 @@ class cos_distill_args(ctypes.Structure):
         ("student", ctypes.c_void_p), ("stride_student", ctypes.c_int64), ("rows", ctypes.c_int32), ("vocab", ctypes.c_int32),
         ("dtype", ctypes.c_int32), ("device", ctypes.c_int32), ("lists", ctypes.c_int32), ("k", ctypes.c_int32),
         ("ids", ctypes.c_void_p), ("values", ctypes.c_void_p), ("lse", ctypes.c_void_p),
-        ("weights", ctypes.c_float * COS_MAX_MODELS), ("temperature", ctypes.c_float), ("row_weights", ctypes.c_void_p),
+        ("weights", ctypes.c_float * COS_MAX_MODELS), ("temperature", ctypes.c_double), ("row_weights", ctypes.c_void_p),
         ("loss", ctypes.c_void_p), ("statistics", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("stride_grad", ctypes.c_int64),
     ]
 

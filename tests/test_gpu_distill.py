@@ -35,7 +35,7 @@ def reference(s, ids, values, lse, weights, T):
     host = lambda v: None if v is None else v.double().cpu().numpy()  # noqa: E731
     s, values, lse = host(s), host(values), host(lse)
     ids = ids.cpu().numpy()
-    T = float(np.float32(T))
+    T = float(T)
     return [distill(s[r], ids[r], values[r], None if lse is None else lse[r], weights, T) for r in range(s.shape[0])], s, T
 
 
@@ -161,7 +161,7 @@ def test_gradient_against_differences():
     s, ids, values, lse = make(1, 300, "f32", 2, 10, seed=8)
     w = [0.3, 0.7]
     grad = pkg.distill_step(s, ids, values, torch.ones(1, device="cuda"), lse, w, 1.3)["grad"][0].double().cpu().numpy()
-    x, t = s[0].double().cpu().numpy(), float(np.float32(1.3))
+    x, t = s[0].double().cpu().numpy(), 1.3
     l64 = lambda y: distill(y, ids[0].cpu().numpy(), values[0].double().cpu().numpy(), lse[0].double().cpu().numpy(), w, t)[0]  # noqa: E731
     for i in [int(ids[0, 0, 0]), int(ids[0, 1, 3]), 5, 99, 299]:
         h = 1e-4

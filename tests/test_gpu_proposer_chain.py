@@ -70,7 +70,7 @@ def test_draft_verify_and_teach(dtype):
     for i in range(n):
         assert torch.allclose(tops[i]["lse"], out["lse"].view(rows, n)[:, i], rtol=1e-5, atol=1e-5)
         for r in range(0, rows, 17):
-            values, ids, _ = top_of(host[i][r], 32, float(np.float32(T)))
+            values, ids, _ = top_of(host[i][r], 32, T)
             assert np.array_equal(tops[i]["ids"][r].cpu().numpy(), ids) and np.array_equal(tops[i]["values"][r].double().cpu().numpy(), values)
     ids, values, lse = (torch.stack([t[k] for t in tops], 1).contiguous() for k in ("ids", "values", "lse"))
     student = before[0].view(rows, V).clone().requires_grad_(True)
@@ -78,6 +78,6 @@ def test_draft_verify_and_teach(dtype):
     grad, = torch.autograd.grad(loss.mean(), student)
     s = student.detach().double().cpu().numpy()
     for r in range(0, rows, 17):
-        l, want, t, q64 = distill(s[r], ids[r].cpu().numpy(), values[r].double().cpu().numpy(), lse[r].double().cpu().numpy(), weights, float(np.float32(T)))
+        l, want, t, q64 = distill(s[r], ids[r].cpu().numpy(), values[r].double().cpu().numpy(), lse[r].double().cpu().numpy(), weights, T)
         check_loss(float(loss[r].detach()), l, t, V)
-        check_grad(grad[r].double().cpu().numpy(), want, q64, t, s[r], float(np.float32(T)), float(np.float32(1.0 / rows)), dtype)
+        check_grad(grad[r].double().cpu().numpy(), want, q64, t, s[r], T, float(np.float32(1.0 / rows)), dtype)

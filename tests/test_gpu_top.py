@@ -18,7 +18,7 @@ def check(x, k, T):
     host = x.double().cpu().numpy()
     got = {n: v.double().cpu().numpy() for n, v in out.items()}
     for r in range(rows):
-        v, ids, lse = top_of(host[r], k, float(np.float32(T)))
+        v, ids, lse = top_of(host[r], k, float(T))
         assert np.array_equal(got["ids"][r], ids), (r, got["ids"][r], ids)
         assert np.array_equal(got["values"][r], v)
         if not math.isfinite(lse):

@@ -3,8 +3,8 @@
 //
 // What bounds small runs called from Python is the call itself: with its steps in Python one row of 5 x 2 x 32000 took 14.8 us a call, of
 // which the device needs 12.4; now it takes 12.8.  Whatever does not fit here (other outputs, tensors that are not plain, anything to
-// complain about) returns None, and the caller goes the long way, which has the messages.  Likewise drawing from one row 18.6 -> 11 us a call, and distillation
-// forward and backward 111 -> 45 us, where the autograd function is a node of the engine's own kind.
+// complain about) returns None, and the caller goes the long way, which has the messages.  Likewise drawing from one row 18.7 -> 9.2 us a call (the device's
+// time), and distillation forward and backward of 16 rows 113 -> 60 us (of which the engine takes 52 for any graph), where the autograd function is a node of the engine's own kind.
 #include <ATen/ops/as_strided.h>
 #include <ATen/ops/empty.h>
 #include <Python.h>

@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(kShareThreads) cos_distill_shares_kernel(const
   extern __shared__ uint4 smem[];
   __shared__ double per_warp[kShareThreads / 32], list_max[COS_MAX_MODELS], list_sum[COS_MAX_MODELS];
   wait_for_inputs();
-  asm volatile("griddepcontrol.launch_dependents;");  // (the rows: they read the student, which is settled where every block has come here)
+  let_next_launch();  // (the rows: they read the student, which is settled where every block has come here)
   const int row = blockIdx.x, n = p.lists * p.k;
   const Shares sh = {reinterpret_cast<double*>(smem), reinterpret_cast<int*>(smem) + 2 * n, reinterpret_cast<float*>(smem) + 3 * n, per_warp, list_max, list_sum};
   const char* student = p.student + static_cast<long long>(row) * p.stride * Elem<DT>::bytes;

@@ -779,6 +779,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
   const int parts = p.c.parts, rank = blockIdx.x & (parts - 1), row = blockIdx.x >> p.c.shift, tid = threadIdx.x;
   if (parts > 1) cluster_barrier_arrive();
   wait_for_inputs();
+  let_next_launch();
   RowSlice<DT> s;
   s.init(static_cast<const char*>(p.c.logits) + static_cast<long long>(row) * p.c.stride * Elem<DT>::bytes, p.c.V, rank, p.c.share, p.c.seg, smem + sizeof(h) / 16, p.c.res);
   s.start();
@@ -1028,6 +1029,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_top_kernel(const TopPara
   const int parts = kStream ? 1 : p.c.parts, rank = kStream ? 0 : blockIdx.x & (parts - 1), row = kStream ? blockIdx.x : blockIdx.x >> p.c.shift, tid = threadIdx.x;
   if (parts > 1) cluster_barrier_arrive();
   wait_for_inputs();
+  let_next_launch();
   RowSlice<DT> s;
   s.init(static_cast<const char*>(p.c.logits) + static_cast<long long>(row) * p.c.stride * Elem<DT>::bytes, p.c.V, rank, p.c.share, p.c.seg, smem + sizeof(h) / 16, p.c.res);
   if (tid < 64) h.steps[tid] = 0;

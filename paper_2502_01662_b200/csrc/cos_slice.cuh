@@ -225,6 +225,9 @@ struct RowSlice {
 
 // Everything that the work ahead in the stream wrote is there (launches take their places while it drains).
 __device__ __forceinline__ void wait_for_inputs() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// Behind that: the next launch may take its places when every block of this one has come here.  (Not sooner: one that starts on inputs which the work just ahead of it does not write
+// relies on what lies before that being complete.)  Saves 0.5 us between small calls of one launch; calls of two lose up to 2.
+__device__ __forceinline__ void let_next_launch() { asm volatile("griddepcontrol.launch_dependents;"); }
 
 // ------------------------------------------------------------------------------------
 // the cluster

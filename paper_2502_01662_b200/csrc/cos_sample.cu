@@ -245,7 +245,7 @@ struct Weight {
 
 struct Found {
   u64 before_count, before_mass, count;
-  int bin, there;
+  int bin, pad;
 };
 
 template <int kList>
@@ -265,11 +265,11 @@ using SampleShared = Shared<kCandidates>;
 static_assert(sizeof(SampleShared) % 16 == 0 && sizeof(Shared<kTopCandidates>) % 16 == 0, "the slice lies behind it");
 
 constexpr int kBinsEach = kBins / kSliceThreads;
-// The bins of this block's share of the row's histogram, with what lies before them in the line.
+static_assert(kBinsEach == 2, "a thread reads two bins at once");
+// The row's histogram: a thread's bins, with what lies before them in the line.
 struct Bins {
-  int first, n;  // this thread's
   u64 count[kBinsEach], mass[kBinsEach], before_count, before_mass;
-  u64 all_count, all_mass;  // of the row
+  u64 all_count, all_mass;
 };
 
 // What is the same for every step of a row.
@@ -285,50 +285,48 @@ __device__ __forceinline__ void clear_bins(H& h) {
   for (int i = threadIdx.x; i < kBins; i += kSliceThreads) h.count[i] = h.lo[i] = h.hi[i] = 0;
 }
 
-// Behind the sweep that filled the blocks' bins and a barrier of the row: the sums over the blocks, in order, with mass_of(bin, count, lo, hi) for a bin.  The
-// bins may be cleared afterwards.
+// Behind the sweep that filled the blocks' bins and a barrier of the row: the sums over the blocks, in order, with mass_of(bin, count, lo, hi) for a bin, of the first `bins`.  Every block reads the bins of all
+// of them (64 KB over 16 blocks at 10 bytes a clock), which takes less than a share for each and telling one another.  Bins may be cleared behind the next barrier of the row.
 template <class H, class M>
-__device__ __forceinline__ void merge_bins(Row<H>& w, bool masses, bool wide, bool packed, Bins& b, M&& mass_of) {
-  const int own = kBins / w.parts, each = own > kSliceThreads ? own / kSliceThreads : 1;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  b.n = tid * each < own ? each : 0;
-  b.first = w.rank * own + tid * each;
+__device__ __forceinline__ void merge_bins(Row<H>& w, int bins, bool masses, bool wide, bool packed, Bins& b, M&& mass_of) {
+  constexpr int kAtOnce = 4;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, first = tid * kBinsEach;
+  unsigned n[2] = {0, 0}, hi[2] = {0, 0};
+  u64 lo[2] = {0, 0};
+  const auto add = [&](const uint2& c, const uint2& l, const uint2& h) {
+    constexpr unsigned kPlaces = (1u << kPackedShift) - 1;
+    n[0] += packed ? c.x >> kPackedShift : c.x;
+    n[1] += packed ? c.y >> kPackedShift : c.y;
+    lo[0] += packed ? c.x & kPlaces : l.x;
+    lo[1] += packed ? c.y & kPlaces : l.y;
+    hi[0] += h.x;
+    hi[1] += h.y;
+  };
+  const auto two = [&](const unsigned (&of)[kBins]) { return *reinterpret_cast<const uint2*>(&of[first]); };
+  const uint2 none = make_uint2(0, 0);
+  if (first >= bins) {
+  } else if (w.parts == 1) {
+    add(two(w.h.count), masses && !packed ? two(w.h.lo) : none, wide ? two(w.h.hi) : none);
+  } else {
+    for (int r0 = 0; r0 < w.parts; r0 += kAtOnce) {  // (so many blocks' under way at once, a block again where there are fewer)
+      uint2 c[kAtOnce], l[kAtOnce], h[kAtOnce];
+#pragma unroll
+      for (int r = 0; r < kAtOnce; ++r) {
+        const H* o = of_rank(&w.h, min(r0 + r, w.parts - 1));
+        c[r] = two(o->count);
+        l[r] = masses && !packed ? two(o->lo) : none;
+        h[r] = wide ? two(o->hi) : none;
+      }
+#pragma unroll
+      for (int r = 0; r < kAtOnce; ++r)
+        if (r0 + r < w.parts) add(c[r], l[r], h[r]);
+    }
+  }
   u64 count = 0, mass = 0;
 #pragma unroll
   for (int q = 0; q < kBinsEach; ++q) {
-    b.count[q] = b.mass[q] = 0;
-    if (q < b.n) {
-      const int i = b.first + q;
-      unsigned n = 0;
-      u64 lo = 0;
-      unsigned hi = 0;
-      if (w.parts == 1) {
-        n = w.h.count[i];
-        lo = packed ? n & ((1u << kPackedShift) - 1) : w.h.lo[i];
-        hi = w.h.hi[i];
-        if (packed) n >>= kPackedShift;
-      } else {
-        for (int first = 0; first < w.parts; first += 8) {  // (eight blocks' under way at once, a block again where there are fewer)
-          unsigned each[8], low[8], high[8];
-#pragma unroll
-          for (int r = 0; r < 8; ++r) {
-            const H* o = of_rank(&w.h, min(first + r, w.parts - 1));
-            each[r] = o->count[i];
-            low[r] = masses && !packed ? o->lo[i] : 0u;
-            high[r] = wide ? o->hi[i] : 0u;
-          }
-#pragma unroll
-          for (int r = 0; r < 8; ++r)
-            if (first + r < w.parts) {
-              n += packed ? each[r] >> kPackedShift : each[r];
-              lo += packed ? each[r] & ((1u << kPackedShift) - 1) : low[r];
-              hi += high[r];
-            }
-        }
-      }
-      b.count[q] = n;
-      if (masses) b.mass[q] = mass_of(i, n, lo, hi);
-    }
+    b.count[q] = n[q];
+    b.mass[q] = masses && first < bins ? mass_of(first + q, n[q], lo[q], hi[q]) : 0;
     count += b.count[q];
     mass += b.mass[q];
   }
@@ -345,16 +343,11 @@ __device__ __forceinline__ void merge_bins(Row<H>& w, bool masses, bool wide, bo
     w.h.scan_count[warp] = sc;
     w.h.scan_mass[warp] = sm;
   }
-  const int t = w.turn & 1;
-  exchange<Add, Add>(w.x, w.turn, w.parts, w.rank, count, mass);  // (its barriers are this scan's too)
-  sc -= count;
-  sm -= mass;
-  // (what the warps and blocks before this one have, and the row: by every warp at once)
-  sc += Add::warp(lane < warp ? w.h.scan_count[lane & (kSliceWarps - 1)] : 0);
-  sm += Add::warp(lane < warp ? w.h.scan_mass[lane & (kSliceWarps - 1)] : 0);
-  const u64 ac = lane < w.parts ? w.x.a[t][lane & (kSliceParts - 1)] : 0, am = lane < w.parts ? w.x.b[t][lane & (kSliceParts - 1)] : 0;
-  b.before_count = sc + Add::warp(lane < w.rank ? ac : 0);
-  b.before_mass = sm + Add::warp(lane < w.rank ? am : 0);
+  __syncthreads();
+  // (what the warps before this one have, and all of them: by every warp at once)
+  const u64 ac = lane < kSliceWarps ? w.h.scan_count[lane & (kSliceWarps - 1)] : 0, am = lane < kSliceWarps ? w.h.scan_mass[lane & (kSliceWarps - 1)] : 0;
+  b.before_count = sc - count + Add::warp(lane < warp ? ac : 0);
+  b.before_mass = sm - mass + Add::warp(lane < warp ? am : 0);
   b.all_count = Add::warp(ac);
   b.all_mass = Add::warp(am);
 }
@@ -365,28 +358,14 @@ __device__ __forceinline__ Found locate(Row<H>& w, const Bins& b, bool by_mass, 
   const int slot = w.slot;
   w.slot ^= 1;
   u64 c = b.before_count, m = b.before_mass;
-  Found f = {0, 0, 0, 0, 0};
 #pragma unroll
   for (int q = 0; q < kBinsEach; ++q) {
     const u64 at = by_mass ? m : c, here = by_mass ? b.mass[q] : b.count[q];
-    if (q < b.n && at < target && target <= at + here) f = {c, m, b.count[q], b.first + q, 1};
+    if (at < target && target <= at + here) w.h.found[slot] = {c, m, b.count[q], static_cast<int>(threadIdx.x) * kBinsEach + q, 0};  // (one thread)
     c += b.count[q];
     m += b.mass[q];
   }
-  const unsigned who = __ballot_sync(0xffffffffu, f.there);
-  if (who) {  // (one lane of the row: its warp tells every block)
-    const int src = __ffs(who) - 1, lane = threadIdx.x & 31;
-    f.before_count = __shfl_sync(0xffffffffu, f.before_count, src);
-    f.before_mass = __shfl_sync(0xffffffffu, f.before_mass, src);
-    f.count = __shfl_sync(0xffffffffu, f.count, src);
-    f.bin = __shfl_sync(0xffffffffu, f.bin, src);
-    if (w.parts == 1) {
-      if (lane == 0) w.h.found[slot] = f;
-    } else if (lane < w.parts) {
-      *of_rank(&w.h.found[slot], lane) = f;
-    }
-  }
-  row_barrier(w.parts);
+  __syncthreads();
   return w.h.found[slot];
 }
 
@@ -472,7 +451,7 @@ __device__ __forceinline__ Range narrow(Row<H>& w, const S& s, W&& weight, bool 
   g.hi = ends.b;
   while (g.count > most) {
     const int bits = 64 - __clzll(static_cast<long long>(g.hi - g.lo)), shift = bits > kBinBits ? bits - kBinBits : 0;
-    __syncthreads();
+    row_barrier(w.parts);  // (the bins have been read by all blocks)
     clear_bins(w.h);
     __syncthreads();
     s.entries([&](int token, float v) {
@@ -490,7 +469,7 @@ __device__ __forceinline__ Range narrow(Row<H>& w, const S& s, W&& weight, bool 
     });
     row_barrier(w.parts);
     Bins b;
-    merge_bins(w, by_mass, by_mass, false, b, [](int, unsigned, u64 lo, unsigned hi) { return (static_cast<u64>(hi) << 32) + lo; });
+    merge_bins(w, kBins, by_mass, by_mass, false, b, [](int, unsigned, u64 lo, unsigned hi) { return (static_cast<u64>(hi) << 32) + lo; });
     const Found sub = locate(w, b, by_mass, target - (by_mass ? g.before_mass : g.before_count));
     g.before_count += sub.before_count;
     g.before_mass += sub.before_mass;
@@ -604,15 +583,15 @@ __device__ __forceinline__ u64 limit_by_count(Row<H>& w, const S& s, W&& weight,
 // ... and by mass: those before which less than `target` lies, 1 <= target <= the mass of the row.  b: the row's bins, whose masses are estimates; bin_at: a
 // logit's bin before it is cut to a whole number.
 template <int DT, class H, class BinAt>
-__device__ __forceinline__ u64 limit_by_mass(Row<H>& w, const RowSlice<DT>& s, const Weight<DT>& weight, u64 target, const Bins& b, BinAt&& bin_at) {
+__device__ __forceinline__ u64 limit_by_mass(Row<H>& w, const RowSlice<DT>& s, const Weight<DT>& weight, u64 target, const Bins& b, int bins, BinAt&& bin_at) {
   const auto weigh = [&](float v) { return weight.of(v); };
   Found f = locate(w, b, true, Max::two(1, Min::two(target, b.all_mass)));
   Range g;
   int n;
   for (;;) {  // the estimates are good to 1e-4: the bin is this one or one next to it
-    const auto in = [&](float v) { return min(static_cast<int>(bin_at(v)), kBins - 1) == f.bin; };
+    const auto in = [&](float v) { return min(static_cast<int>(bin_at(v)), bins - 1) == f.bin; };
     const float lo = static_cast<float>(f.bin), hi = lo + 1.0f;
-    const bool last_bin = f.bin == kBins - 1;
+    const bool last_bin = f.bin == bins - 1;
     const bool few = f.count <= kCandidates;
     u64 above = 0, inside = 0;
     s.raw([&](int token, const uint4& r) {
@@ -896,27 +875,29 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
         return;
       }
     }
-    // Bins of 1/64 of a logit for a top-k alone, of 1/32 of a power of two of the weight for both.  For a top-p alone they reach as far as its limit may lie: all logits
+    // Bins of 1/64 of a logit for a top-k alone, of 1/32 of a power of two of the weight for both (twice that where there are 512).  For a top-p alone they reach as far as its limit may lie: all logits
     // whose weight is below (1 - p) / vocab of the total have less than (1 - p) of it together, and are left out.
+    // 512 bins over 16 blocks, whose bins take 7000 clocks to read otherwise.
+    const int bins = parts > 8 ? kBins / 2 : kBins;
     bool cut = false;
-    float per_unit = 32.0f;
+    float per_unit = static_cast<float>(bins / 32);
     if (by_p && !by_k) {
       const double at = (1.0 - static_cast<double>(fmaxf(top_p, 0.0f))) * static_cast<double>(total) / p.c.V;  // that weight, in units
       cut = at >= 16.0;                                                                                      // (far from the rounding to units)
-      if (cut) per_unit = static_cast<float>(kBins - 2) / fmaxf(static_cast<float>(weight.scale) - log2f(static_cast<float>(at)) + 0.1f, 0.01f);
+      if (cut) per_unit = static_cast<float>(bins - 2) / fmaxf(static_cast<float>(weight.scale) - log2f(static_cast<float>(at)) + 0.1f, 0.01f);
     }
-    const float per_half = by_p ? fminf(per_unit * weight.c32x2, 1e30f) : 128.0f;
+    const float per_half = by_p ? fminf(per_unit * weight.c32x2, 1e30f) : static_cast<float>(bins / 8);
     const auto bin_at = [&](float v) { return fmaf(-0.5f, v, weight.half) * per_half; };
-    const auto bin_of = [&](float v) { return min(static_cast<int>(bin_at(v)), kBins - 1); };
+    const auto bin_of = [&](float v) { return min(static_cast<int>(bin_at(v)), bins - 1); };
     const bool packed = by_p && p.c.share <= kPackedEntries / Elem<DT>::E;
     s.raw([&](int, const uint4& r) {
 #pragma unroll
       for (int e = 0; e < Elem<DT>::E; ++e) {
         const float v = entry<DT>(r, e);
         const int eighths = static_cast<int>(bin_at(v) * 8.0f), bin = eighths >> 3;
-        if (v > -INFINITY && (bin < kBins - 1 || !cut)) {
-          const unsigned part = by_p && bin < kBins - 1 ? eighths & 7 : 0;
-          atomicAdd(&h.count[min(bin, kBins - 1)], packed ? 1u << kPackedShift | part : 1u);
+        if (v > -INFINITY && (bin < bins - 1 || !cut)) {
+          const unsigned part = by_p && bin < bins - 1 ? eighths & 7 : 0;
+          atomicAdd(&h.count[min(bin, bins - 1)], packed ? 1u << kPackedShift | part : 1u);
           if (!packed && part) atomicAdd(&h.lo[bin], part);
         }
       }
@@ -926,9 +907,9 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
     // the weights of a bin, from the places of its tokens in it (in eighths), up to the curvature of exp2 over it (1e-4)
     const float eighth = (1.0f - exp2f(-1.0f / per_unit)) * 0.125f;
     const double unit = weight.power(0);
-    merge_bins(w, by_p, false, packed, b, [&](int bin, unsigned count, u64 eighths, unsigned) {
+    merge_bins(w, bins, by_p, false, packed, b, [&](int bin, unsigned count, u64 eighths, unsigned) {
       const float part = static_cast<float>(count) - eighth * (static_cast<float>(eighths) + 0.5f * static_cast<float>(count));
-      return bin == kBins - 1 ? 0ull : static_cast<u64>(unit * static_cast<double>(part * exp2f(static_cast<float>(-bin) / per_unit)));
+      return bin == bins - 1 ? 0ull : static_cast<u64>(unit * static_cast<double>(part * exp2f(static_cast<float>(-bin) / per_unit)));
     });
     if (by_k && static_cast<u64>(k) < b.all_count) {
       const Found f = locate(w, b, false, k);
@@ -943,7 +924,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
         total = exchange<Add>(x, w.turn, parts, rank, mine).a;
       }
       const u64 target = share_of(total);
-      if (target < total) last = Max::two(last, limit_by_mass<DT>(w, s, weight, target, b, bin_at));
+      if (target < total) last = Max::two(last, limit_by_mass<DT>(w, s, weight, target, b, bins, bin_at));
     }
   }
 
@@ -1117,7 +1098,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_top_kernel(const TopPara
     });
     row_barrier(parts);
     Bins b;
-    merge_bins(w, false, false, false, b, [](int, unsigned, u64, unsigned) { return 0ull; });
+    merge_bins(w, kBins, false, false, false, b, [](int, unsigned, u64, unsigned) { return 0ull; });
     u64 from = 0;  // of places
     if (static_cast<u64>(p.k) < b.all_count) {
       const Found f = locate(w, b, false, p.k);

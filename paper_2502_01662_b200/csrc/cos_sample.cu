@@ -195,6 +195,14 @@ struct Weight {
     for (unsigned e = kept & ~close; e; e &= e - 1) sum += far(pick(r, __ffs(e) - 1));
     return sum;
   }
+  // Sum over all entries of a vector.
+  __device__ __forceinline__ u64 of_entries(const uint4& r) const {
+    unsigned head = 0, as_far = 0;
+#pragma unroll
+    for (int e = 0; e < Elem<DT>::E; ++e) head |= static_cast<unsigned>(entry<DT>(r, e) >= near_from) << e;
+    const u64 sum = near_ones(r, head, as_far);
+    return sum + static_cast<unsigned>(far_vector(r) - as_far);  // (modulo 2^32)
+  }
   // Sum over all entries of this lane.  Vectors far below the largest go by 32 bits; those with near entries in a second pass, in which every lane goes from one of its own to
   // the next (few where the tail is long): the near ones by 64-bit instructions, the others by 32 bits with all of the vector, modulo 2^32, from which what that makes
   // of the near ones is taken off again.
@@ -934,7 +942,8 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
   const auto keeps = [&](float v, int token) { return (v > bound) | ((v == bound) & (token <= last_token)); };
   u64 mine = 0;
   unsigned kept = 0;
-  if (last == everything && bound == last_logit) {
+  const bool every = last == everything && bound == last_logit;
+  if (every) {
     mine = weight.of_all(s, kept);
   } else if (own >= bound) {
     s.raw([&](int token, const uint4& r) {
@@ -962,7 +971,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
         const int i = at + lane;
         const uint4 r = i < s.end ? s.at(i) : neg_inf_vector<DT>();
         const int token = s.token(i);
-        const u64 sum = weight.of_vector(r, token, keeps);
+        const u64 sum = every ? weight.of_entries(r) : weight.of_vector(r, token, keeps);
         u64 up = sum;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -970,22 +979,23 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
           if (lane >= d) up += o;
         }
         const unsigned reached = __ballot_sync(0xffffffffu, before + up >= goal);
-        if (reached) {
-          if (lane == __ffs(reached) - 1) {
-            before += up - sum;
-            bool open = true;
+        if (reached) {  // a lane for each entry of that vector
+          const int src = __ffs(reached) - 1;
+          before += __shfl_sync(0xffffffffu, up - sum, src);
+          const uint4 v4 = make_uint4(__shfl_sync(0xffffffffu, r.x, src), __shfl_sync(0xffffffffu, r.y, src), __shfl_sync(0xffffffffu, r.z, src), __shfl_sync(0xffffffffu, r.w, src));
+          const int x0 = __shfl_sync(0xffffffffu, token, src) + lane;
+          const float v = Weight<DT>::pick(v4, lane & (RowSlice<DT>::E - 1));
+          const u64 own_weight = lane < RowSlice<DT>::E && keeps(v, x0) ? weigh(v) : 0;
+          u64 to = own_weight;
 #pragma unroll
-            for (int e = 0; e < RowSlice<DT>::E; ++e) {
-              const float v = entry<DT>(r, e);
-              if (open && keeps(v, token + e)) {
-                before += weigh(v);
-                if (before >= goal) {
-                  open = false;
-                  p.tokens[row] = token + e;
-                  if (p.prob) p.prob[row] = static_cast<float>(weight.exact(v) / static_cast<double>(all.a));
-                }
-              }
-            }
+          for (int d = 1; d < RowSlice<DT>::E; d <<= 1) {
+            const u64 o = __shfl_up_sync(0xffffffffu, to, d);
+            if (lane >= d) to += o;
+          }
+          const unsigned there = __ballot_sync(0xffffffffu, before + to >= goal);
+          if (lane == __ffs(there) - 1) {
+            p.tokens[row] = x0;
+            if (p.prob) p.prob[row] = static_cast<float>(weight.exact(v) / static_cast<double>(all.a));
           }
           break;
         }

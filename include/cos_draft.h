@@ -26,7 +26,7 @@ extern "C" {
 
 typedef struct {
   const void* logits;     /* [rows][vocab], element (r, x) at r * stride_row + x (in elements)          */
-  int64_t stride_row;     /* >= vocab where rows > 1                                                    */
+  int64_t stride_row;     /* >= vocab where rows > 1, or 0: all rows are the same one                   */
   int32_t rows, vocab;    /* >= 1                                                                       */
   int32_t dtype;          /* COS_DTYPE_* of the logits                                                  */
   int32_t device;         /* CUDA device ordinal                                                        */
@@ -89,7 +89,7 @@ cos_status cos_top_logits(const cos_top_args* args, void* cuda_stream);
 
 typedef struct {
   const void* student;    /* [rows][vocab] logits, element (n, x) at n * stride_student + x             */
-  int64_t stride_student; /* >= vocab where rows > 1                                                    */
+  int64_t stride_student; /* >= vocab where rows > 1, or 0: all rows are the same one                   */
   int32_t rows, vocab;    /* >= 1                                                                       */
   int32_t dtype;          /* COS_DTYPE_* of the student's logits and of their gradient                  */
   int32_t device;         /* CUDA device ordinal                                                        */

@@ -411,7 +411,7 @@ cos_status distill(const cos_distill_args* a, void* cuda_stream) {
   if (!a->student || !a->ids || !a->values) return call_failed(COS_ERR_INVALID_ARG, "null device pointer");
   if (a->rows < 1 || a->vocab < 1 || a->vocab > 0x7ffffff0) return call_failed(COS_ERR_INVALID_ARG, "rows and vocab must be positive");
   if (a->dtype < COS_DTYPE_F32 || a->dtype > COS_DTYPE_F16) return call_failed(COS_ERR_INVALID_ARG, "unknown dtype");
-  if (a->rows > 1 && a->stride_student < a->vocab) return call_failed(COS_ERR_INVALID_ARG, "rows overlap: stride_student is less than vocab");
+  if (a->rows > 1 && a->stride_student < a->vocab && a->stride_student != 0) return call_failed(COS_ERR_INVALID_ARG, "rows overlap: stride_student is less than vocab");
   if (a->lists < 1 || a->lists > COS_MAX_MODELS || a->k < 1 || a->k > COS_TOP_MAX || a->lists * a->k > COS_TOP_MAX)
     return call_failed(COS_ERR_INVALID_ARG, "lists must be in [1, COS_MAX_MODELS] and lists * k in [1, COS_TOP_MAX]");
   for (int g = 0; g < a->lists; ++g)

@@ -1165,7 +1165,7 @@ cos_status check_rows(const void* logits, long long stride, int rows, int vocab,
   if (!logits) return call_failed(COS_ERR_INVALID_ARG, "null device pointer");
   if (rows < 1 || vocab < 1 || vocab > 0x7ffffff0) return call_failed(COS_ERR_INVALID_ARG, "rows and vocab must be positive");
   if (dtype < COS_DTYPE_F32 || dtype > COS_DTYPE_F16) return call_failed(COS_ERR_INVALID_ARG, "unknown dtype");
-  if (rows > 1 && stride < vocab) return call_failed(COS_ERR_INVALID_ARG, "rows overlap: stride_row is less than vocab");
+  if (rows > 1 && stride < vocab && stride != 0) return call_failed(COS_ERR_INVALID_ARG, "rows overlap: stride_row is less than vocab");
   if (reinterpret_cast<uintptr_t>(logits) % (dtype == COS_DTYPE_F32 ? 4 : 2)) return call_failed(COS_ERR_ALIGNMENT, "logits pointer not aligned to its element type");
   return COS_OK;
 }

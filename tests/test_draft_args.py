@@ -66,7 +66,7 @@ CASES = [
     *[(_sample(**kw), st) for kw, st in (
         (dict(logits=None), 1), (dict(uniforms=None), 1), (dict(tokens=None), 1), (dict(rows=0), 1), (dict(vocab=0), 1), (dict(rows=-1), 1), (dict(dtype=3), 1), (dict(dtype=-1), 1),
         (dict(stride_row=99), 1), (dict(stride_row=-100), 1), (dict(temperature=-1.0), 1), (dict(temperature=NAN), 1), (dict(top_p=0.0), 1), (dict(top_p=NAN), 1), (dict(min_p=-0.1), 1),
-        (dict(min_p=1.1), 1), (dict(min_p=NAN), 1), (dict(filtered=A + (1 << 19), stride_filtered=50), 1), (dict(filtered=A, stride_filtered=200), 1), (dict(logits=A + 2), 3), (dict(uniforms=A + 1), 3),
+        (dict(min_p=1.1), 1), (dict(min_p=NAN), 1), (dict(filtered=A + (1 << 19), stride_filtered=50), 1), (dict(filtered=A, stride_filtered=200), 1), (dict(stride_row=0, filtered=A, stride_filtered=100), 1), (dict(logits=A + 2), 3), (dict(uniforms=A + 1), 3),
         (dict(row_top_k=A + 2), 3), (dict(prob=A + 2), 3), (dict(filtered=A + 1, stride_filtered=100), 3))],
     *[(_top(**kw), st) for kw, st in (
         (dict(logits=None), 1), (dict(values=None), 1), (dict(ids=None), 1), (dict(lse=None), 1), (dict(k=0), 1), (dict(k=101), 1), (dict(vocab=5000, stride_row=5000, k=1025), 1), (dict(temperature=0.0), 1),
@@ -77,7 +77,7 @@ CASES = [
         (dict(lse=A + 2), 3))],
     *[(_distill(name, **kw), st) for name, kw, st in (
         ("cos_distill_loss", dict(loss=None), 1), ("cos_distill_loss", dict(statistics=None), 1), ("cos_distill_loss", dict(statistics=A + 4), 3), ("cos_distill_grad", dict(statistics=None), 1),
-        ("cos_distill_grad", dict(row_weights=None), 1), ("cos_distill_grad", dict(grad=None), 1), ("cos_distill_grad", dict(grad=A + 1), 3), ("cos_distill_step", dict(loss=None), 1),
+        ("cos_distill_step", dict(stride_student=0, grad=A), 1), ("cos_distill_grad", dict(row_weights=None), 1), ("cos_distill_grad", dict(grad=None), 1), ("cos_distill_grad", dict(grad=A + 1), 3), ("cos_distill_step", dict(loss=None), 1),
         ("cos_distill_step", dict(grad=None), 1), ("cos_distill_step", dict(stride_grad=99), 1), ("cos_distill_step", dict(grad=A, stride_grad=101), 1))],
 ]
 

@@ -194,6 +194,22 @@ def test_autograd():
         first.sum().backward()
 
 
+def test_a_student_row_that_is_broadcast():
+    """One row of logits against many lists: the gradients of all of them add up in it."""
+    s, ids, values, lse = make(7, 3001, "f32", 1, 20, seed=16)
+    leaf = s[:1].clone().requires_grad_(True)
+    loss = pkg.distill_loss(leaf.expand(7, 3001), ids, values, lse)
+    rw = torch.rand(7, generator=torch.Generator("cuda").manual_seed(1), device="cuda")
+    grad, = torch.autograd.grad(loss, leaf, rw)
+    want = pkg.distill_step(s[:1].repeat(7, 1), ids, values, rw, lse)
+    again = pkg.distill_step(s[:1].expand(7, 3001), ids, values, rw, lse)
+    assert torch.equal(want["grad"], again["grad"]) and torch.equal(want["loss"], again["loss"])
+    same = s[:1].repeat(7, 1).requires_grad_(True)
+    each, = torch.autograd.grad(pkg.distill_loss(same, ids, values, lse), same, rw)
+    # seven terms added in some order: 6 roundings of at most the sum of their sizes
+    assert bool(((grad - each.double().sum(0, keepdim=True)).abs() <= 6 * 2.0 ** -24 * each.double().abs().sum(0, keepdim=True) + 1e-37).all())
+
+
 def test_rows_longer_than_shared_memory():
     check(*make(2, 700_001, "f32", 1, 64, seed=10, pad=1), [1.0], 1.0)
 

@@ -70,6 +70,17 @@ def test_rows_of_their_own_parameters(dtype):
     run(x, u, T, k, p, m)
 
 
+def test_one_row_for_many_draws():
+    """A row that is broadcast: a uniform and limits of its own for each draw."""
+    x, _ = make(1, 5001, "bf16", seed=31)
+    g = torch.Generator("cuda").manual_seed(31)
+    u = torch.rand(64, generator=g, device="cuda")
+    k = torch.randint(0, 300, (64,), generator=g, device="cuda").int()
+    run(x.expand(64, 5001), u, 0.9, k, 0.95)
+    with pytest.raises(pkg.CosVerifyError):
+        pkg.sample(x.expand(64, 5001), u, filtered=x.expand(64, 5001))
+
+
 def test_bad_parameters_of_rows_are_reported():
     x, u = make(6, 500, "f32", seed=3)
     T = torch.tensor([1.0, -1.0, float("nan"), 0.5, float("inf"), 1e-30], device="cuda")

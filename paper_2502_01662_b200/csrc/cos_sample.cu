@@ -757,19 +757,63 @@ __device__ __forceinline__ float reached_by(H& h, const Groups& g, const float (
   return __double2float_rd(static_cast<double>(g.largest) - (static_cast<double>(step) + 0.01) * static_cast<double>(span) / 64.0);
 }
 
-template <int DT>
+// A row that a block has for itself and that stays in memory: two groups a thread, halves of its vectors.
+constexpr int kOwnGroups = 2;
+__device__ __forceinline__ int group_span(const Common& c) { return (c.seg / 32 + kOwnGroups - 1) / kOwnGroups * 32; }  // vectors of a warp's groups of one half
+// The largest logits of the thread's groups, from one pass over the row; f(four vectors, the largest of them) on the way.
+template <int DT, class H, class F>
+__device__ __forceinline__ Groups stream_groups(H& h, const RowSlice<DT>& s, const Common& c, float (&own)[kOwnGroups], F&& f) {
+  const int half = group_span(c);
+#pragma unroll
+  for (int g = 0; g < kOwnGroups; ++g) {
+    RunningMax<DT> group;
+    s.stream(s.begin + (threadIdx.x & 31) + g * half, min(s.end, s.begin + (g + 1) * half), [&](const uint4 (&r)[4]) {
+      RunningMax<DT> top;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) top.add(r[k]);
+      group.add(top);
+      f(r, top);
+    });
+    own[g] = group.value();
+  }
+  Groups groups;
+  groups.own = max_nan(own[0], own[1]);
+  groups.group = 0.0f;
+  group_range(h, groups, groups.own, own[0] == -INFINITY ? own[1] : own[1] == -INFINITY ? own[0] : fminf(own[0], own[1]));
+  return groups;
+}
+// ... and the candidates from a logit on: the groups with any are dealt out over the warps, whose lanes read a group's vectors side by side.  (h.hits is 0; h.group is free.)
+template <int DT, class H>
+__device__ __forceinline__ void list_groups(H& h, const RowSlice<DT>& s, const Common& c, const float (&own)[kOwnGroups], float from) {
+  const int tid = threadIdx.x, half = group_span(c);
+  unsigned short* const hit = reinterpret_cast<unsigned short*>(h.group);
+  static_assert(sizeof(h.group) >= kOwnGroups * kSliceThreads * sizeof(unsigned short), "a place for every group");
+#pragma unroll
+  for (int g = 0; g < kOwnGroups; ++g)
+    if (own[g] >= from) hit[atomicAdd(&h.hits, 1)] = static_cast<unsigned short>(tid * kOwnGroups + g);
+  __syncthreads();
+  const int hits = h.hits;
+  for (int q = tid >> 5; q < hits; q += kSliceWarps) {
+    const int thread = hit[q] / kOwnGroups, g = hit[q] % kOwnGroups;
+    const int begin = min(s.nv, (thread >> 5) * c.seg), end = min(min(s.nv, begin + c.seg), begin + (g + 1) * half);
+    for (int i = begin + g * half + (thread & 31) + 32 * (tid & 31); i < end; i += 32 * 32) list_from<DT>(h, from, s.token(i), s.fetch(i));
+  }
+}
+
+// kStream: a block for each row, which stays in memory (a top-k that the head is tried for).
+template <int DT, bool kStream>
 __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const SampleParams p) {
   extern __shared__ uint4 smem[];
   SampleShared& h = *reinterpret_cast<SampleShared*>(smem);
   __shared__ Exchange x;
   __shared__ double table[kTable];
-  const int parts = p.c.parts, rank = blockIdx.x & (parts - 1), row = blockIdx.x >> p.c.shift, tid = threadIdx.x;
+  const int parts = kStream ? 1 : p.c.parts, rank = kStream ? 0 : blockIdx.x & (parts - 1), row = kStream ? blockIdx.x : blockIdx.x >> p.c.shift, tid = threadIdx.x;
   if (parts > 1) cluster_barrier_arrive();
   wait_for_inputs();
   let_next_launch();
   RowSlice<DT> s;
-  s.init(static_cast<const char*>(p.c.logits) + static_cast<long long>(row) * p.c.stride * Elem<DT>::bytes, p.c.V, rank, p.c.share, p.c.seg, smem + sizeof(h) / 16, p.c.res);
-  s.start();
+  s.init(static_cast<const char*>(p.c.logits) + static_cast<long long>(row) * p.c.stride * Elem<DT>::bytes, p.c.V, rank, p.c.share, p.c.seg, smem + sizeof(h) / 16, kStream ? 0 : p.c.res);
+  if (!kStream) s.start();
   const float T = p.row_T ? p.row_T[row] : p.T;
   int k = p.row_k ? p.row_k[row] : p.k;
   const float top_p = p.row_p ? p.row_p[row] : p.p, min_p = p.row_min_p ? p.row_min_p[row] : p.min_p;
@@ -778,9 +822,14 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
   table[tid] = exp2(static_cast<double>(tid) / kTable + Weight<DT>::scale_of(p.c.V));
   clear_bins(h);
   if (tid < 64) h.steps[tid] = 0;
-  if (tid == 0) h.listed = 0;
+  if (tid == 0) h.listed = h.hits = 0;
   Row<SampleShared> w = {h, x, parts, rank, 0, 0};
-  const Groups groups = group_max(w, s);
+  Groups groups;
+  float of_groups[kOwnGroups];
+  if constexpr (kStream)
+    groups = stream_groups<DT>(h, s, p.c, of_groups, [](const uint4 (&)[4], const RunningMax<DT>&) {});
+  else
+    groups = group_max(w, s);
   const float m = groups.largest, own = groups.own;
 
   if (!(m > -INFINITY && m < INFINITY) || !(T >= 0.0f)) {
@@ -831,11 +880,17 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
   if (by_k || by_p) {
     u64 total = 0;  // what top-p is a part of
     if (!by_k || k <= kHeadMost) {
-      const float from = reached_by(h, groups, {groups.group}, by_k ? k : min(kHeadGuess, p.c.V));
+      float from;
+      if constexpr (kStream)
+        from = reached_by(h, groups, of_groups, by_k ? k : min(kHeadGuess, p.c.V));
+      else
+        from = reached_by(h, groups, {groups.group}, by_k ? k : min(kHeadGuess, p.c.V));
       u64 sum = 0, mass = 0;
       unsigned unused = 0;
       if (!by_k) sum = weight.of_all(s, unused);
-      if (own >= from) {
+      if (kStream && by_k) {
+        list_groups<DT>(h, s, p.c, of_groups, from);
+      } else if (own >= from) {
         s.raw([&](int token, const uint4& r) {
           const unsigned in = list_from<DT>(h, from, token, r);
           if (!by_k)
@@ -1016,7 +1071,6 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_top_kernel(const TopPara
   extern __shared__ uint4 smem[];
   Shared<kList>& h = *reinterpret_cast<Shared<kList>*>(smem);
   __shared__ Exchange x;
-  constexpr int kGroups = kStream ? 2 : 1;  // of a thread
   const int parts = kStream ? 1 : p.c.parts, rank = kStream ? 0 : blockIdx.x & (parts - 1), row = kStream ? blockIdx.x : blockIdx.x >> p.c.shift, tid = threadIdx.x;
   if (parts > 1) cluster_barrier_arrive();
   wait_for_inputs();
@@ -1027,27 +1081,14 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_top_kernel(const TopPara
   if (tid == 0) h.listed = h.hits = 0;
   Row<Shared<kList>> w = {h, x, parts, rank, 0, 0};
   const float c = p.scale;
-  const int half = (p.c.seg / 32 + kGroups - 1) / kGroups * 32;  // vectors of a warp's groups
   Groups groups;
-  float own[kGroups], mine;  // the largest of this thread's groups, and of them
+  float own[kStream ? kOwnGroups : 1], mine;  // the largest of this thread's groups, and of them
   double sum = 0.0;
   if constexpr (kStream) {
     RunningSum<DT> part;
-#pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-      RunningMax<DT> group;
-      s.stream(s.begin + (tid & 31) + g * half, min(s.end, s.begin + (g + 1) * half), [&](const uint4 (&r)[4]) {
-        RunningMax<DT> top;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) top.add(r[k]);
-        group.add(top);
-        part.add(r, top, c);
-      });
-      own[g] = group.value();
-    }
+    groups = stream_groups<DT>(h, s, p.c, own, [&](const uint4 (&r)[4], const RunningMax<DT>& top) { part.add(r, top, c); });
     mine = part.m;
     sum = part.z;
-    group_range(h, groups, mine, own[0] == -INFINITY ? own[1] : own[1] == -INFINITY ? own[0] : fminf(own[0], own[1]));
   } else {
     s.start();
     groups = group_max(w, s);
@@ -1077,18 +1118,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_top_kernel(const TopPara
   if (p.k <= kHeadMost) {
     const float from = reached_by(h, groups, own, p.k);
     if constexpr (kStream) {
-// the groups with candidates are dealt out over the warps, whose lanes read a group's vectors side by side
-      unsigned short* const hit = reinterpret_cast<unsigned short*>(h.group);
-#pragma unroll
-      for (int g = 0; g < kGroups; ++g)
-        if (own[g] >= from) hit[atomicAdd(&h.hits, 1)] = static_cast<unsigned short>(tid * kGroups + g);
-      __syncthreads();
-      const int hits = h.hits;
-      for (int q = tid >> 5; q < hits; q += kSliceWarps) {
-        const int thread = hit[q] / kGroups, g = hit[q] % kGroups;
-        const int begin = min(s.nv, (thread >> 5) * p.c.seg), end = min(min(s.nv, begin + p.c.seg), begin + (g + 1) * half);
-        for (int i = begin + g * half + (thread & 31) + 32 * (tid & 31); i < end; i += 32 * 32) list_from<DT>(h, from, s.token(i), s.fetch(i));
-      }
+list_groups<DT>(h, s, p.c, own, from);
     } else if (mine >= from) {
       s.raw([&](int token, const uint4& r) { list_from<DT>(h, from, token, r); });
     }
@@ -1169,6 +1199,10 @@ cos_status check_rows(const void* logits, long long stride, int rows, int vocab,
   if (reinterpret_cast<uintptr_t>(logits) % (dtype == COS_DTYPE_F32 ? 4 : 2)) return call_failed(COS_ERR_ALIGNMENT, "logits pointer not aligned to its element type");
   return COS_OK;
 }
+
+// A block for each row where there are rows enough and one does not fit into a block's shared memory (top 64 of 64 rows of 128256 bf16 13.0 us, on clusters 14.0; of 256 19.9 and 47;
+// of 32 12.7 and 10.2; of 256 rows of 8000 12.7 and 7.3).
+bool own_blocks(int rows, int vocab, int dtype) { return rows >= 48 && static_cast<long long>(vocab) * (dtype == COS_DTYPE_F32 ? 4 : 2) > kMostKept; }
 
 template <class P, class F>
 cos_status launch_rows(P& p, int rows, int vocab, int dtype, int device, size_t shared, bool whole, cudaStream_t stream, F&& kernel_of) {
@@ -1255,9 +1289,15 @@ extern "C" cos_status cos_sample(const cos_sample_args* a, void* cuda_stream) {
   p.status = a->row_status;
   p.filtered = static_cast<char*>(a->filtered);
   p.stride_filtered = a->stride_filtered;
-  return launch_rows(p, a->rows, a->vocab, a->dtype, a->device, sizeof(SampleShared), false, static_cast<cudaStream_t>(cuda_stream), [](int dt) {
-    return dt == COS_DTYPE_F32 ? cos_sample_kernel<COS_DTYPE_F32> : (dt == COS_DTYPE_BF16 ? cos_sample_kernel<COS_DTYPE_BF16> : cos_sample_kernel<COS_DTYPE_F16>);
-  });
+  const auto call = [&](auto stream) {
+    constexpr bool kStream = decltype(stream)::value;
+    return launch_rows(p, a->rows, a->vocab, a->dtype, a->device, sizeof(SampleShared), kStream, static_cast<cudaStream_t>(cuda_stream), [](int dt) {
+      return dt == COS_DTYPE_F32 ? cos_sample_kernel<COS_DTYPE_F32, kStream> : (dt == COS_DTYPE_BF16 ? cos_sample_kernel<COS_DTYPE_BF16, kStream> : cos_sample_kernel<COS_DTYPE_F16, kStream>);
+    });
+  };
+  // A block for each row as for top logits, where the host knows that the rows are done with their heads.
+  const bool head = !a->row_top_k && !a->row_temperature && a->temperature > 0.0f && a->top_k > 0 && a->top_k <= kHeadMost && a->top_k < a->vocab;
+  return head && own_blocks(a->rows, a->vocab, a->dtype) ? call(std::true_type()) : call(std::false_type());
 }
 
 extern "C" cos_status cos_top_logits(const cos_top_args* a, void* cuda_stream) {
@@ -1286,8 +1326,5 @@ extern "C" cos_status cos_top_logits(const cos_top_args* a, void* cuda_stream) {
   };
   using Few = std::integral_constant<int, kCandidates>;
   if (a->k > kMost<kCandidates>) return call(std::integral_constant<int, kTopCandidates>(), std::false_type());
-  // A block for each row where there are rows enough and one does not fit into a block's shared memory (top 64 of 64 rows of 128256 bf16 13.0 us, on clusters 14.0; of 256 19.9 and 47;
-  // of 32 12.7 and 10.2; of 256 rows of 8000 12.7 and 7.3).
-  const bool long_rows = static_cast<long long>(a->vocab) * (a->dtype == COS_DTYPE_F32 ? 4 : 2) > kMostKept;
-  return a->rows >= 48 && long_rows ? call(Few(), std::true_type()) : call(Few(), std::false_type());
+  return own_blocks(a->rows, a->vocab, a->dtype) ? call(Few(), std::true_type()) : call(Few(), std::false_type());
 }

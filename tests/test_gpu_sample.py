@@ -257,3 +257,29 @@ def test_every_token_is_drawn_as_often_as_its_weight_says():
     law[line[:n]] = w[line[:n]] / w[line[:n]].sum()
     counts = np.bincount(out["tokens"].cpu().numpy(), minlength=V)
     assert np.all(np.abs(counts - N * law) <= 1.0 + 1e-6), (counts, N * law)     # N law uniforms lie in a token's part, to within one at either end
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_many_long_rows(dtype):
+    """Rows enough for a block each, longer than its shared memory: masks, ties and rows that are not finite among ordinary ones, unaligned."""
+    rows, V = 61, 40001
+    x, u = make(rows, V, dtype, seed=17, pad=1)
+    inf = float("inf")
+    g = torch.Generator("cuda").manual_seed(18)
+    x[1] = 0.5
+    x[2] = -inf
+    x[3, 10:] = -inf
+    x[4, 5] = float("nan")
+    x[5, 7] = inf
+    x[6] = torch.finfo(x.dtype).min
+    x[7, 1:] = torch.finfo(x.dtype).min
+    x[8] = torch.randint(0, 3, (V,), generator=g, device="cuda").to(x.dtype)
+    x[9] = torch.linspace(-20, 20, V, device="cuda").to(x.dtype)
+    x[10, ::2] = -inf
+    for T, k, p, least in ((1.0, 50, 1.0, 0.0), (0.7, 288, 0.9, 0.0), (1.3, 1, 1.0, 0.0), (0.9, 100, 0.5, 0.05), (1.0, 289, 0.9, 0.0)):
+        run(x, u, T, k, p, least)
+    want = run(x, u, 0.8, 60, 0.95, 0.01)
+    kept = x.as_strided((rows, 1), (V + 1, 1), V).clone()
+    got = pkg.sample(x, u, 0.8, 60, 0.95, 0.01, filtered=x)
+    assert torch.equal(torch.nan_to_num(x.float(), nan=-7.0), torch.nan_to_num(want["filtered"].float(), nan=-7.0)) and torch.equal(got["tokens"], want["tokens"])
+    assert torch.equal(x.as_strided((rows, 1), (V + 1, 1), V), kept)

@@ -782,9 +782,10 @@ __device__ __forceinline__ Groups stream_groups(H& h, const RowSlice<DT>& s, con
   group_range(h, groups, groups.own, own[0] == -INFINITY ? own[1] : own[1] == -INFINITY ? own[0] : fminf(own[0], own[1]));
   return groups;
 }
-// ... and the candidates from a logit on: the groups with any are dealt out over the warps, whose lanes read a group's vectors side by side.  (h.hits is 0; h.group is free.)
-template <int DT, class H>
-__device__ __forceinline__ void list_groups(H& h, const RowSlice<DT>& s, const Common& c, const float (&own)[kOwnGroups], float from) {
+// ... and f(token of the first entry, vector) for the vectors of the groups that reach a logit: those groups are dealt out over the warps, whose lanes read a group's vectors side by side.
+// (Once a launch: h.hits is 0; h.group is free.)
+template <int DT, class H, class F>
+__device__ __forceinline__ void in_groups(H& h, const RowSlice<DT>& s, const Common& c, const float (&own)[kOwnGroups], float from, F&& f) {
   const int tid = threadIdx.x, half = group_span(c);
   unsigned short* const hit = reinterpret_cast<unsigned short*>(h.group);
   static_assert(sizeof(h.group) >= kOwnGroups * kSliceThreads * sizeof(unsigned short), "a place for every group");
@@ -796,11 +797,11 @@ __device__ __forceinline__ void list_groups(H& h, const RowSlice<DT>& s, const C
   for (int q = tid >> 5; q < hits; q += kSliceWarps) {
     const int thread = hit[q] / kOwnGroups, g = hit[q] % kOwnGroups;
     const int begin = min(s.nv, (thread >> 5) * c.seg), end = min(min(s.nv, begin + c.seg), begin + (g + 1) * half);
-    for (int i = begin + g * half + (thread & 31) + 32 * (tid & 31); i < end; i += 32 * 32) list_from<DT>(h, from, s.token(i), s.fetch(i));
+    for (int i = begin + g * half + (thread & 31) + 32 * (tid & 31); i < end; i += 32 * 32) f(s.token(i), s.fetch(i));
   }
 }
 
-// kStream: a block for each row, which stays in memory (a top-k that the head is tried for).
+// kStream: a block for each row, which stays in memory (a temperature of 0, or a top-k that the head is tried for).
 template <int DT, bool kStream>
 __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const SampleParams p) {
   extern __shared__ uint4 smem[];
@@ -845,9 +846,15 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
 
   if (T == 0.0f) {
     u64 first = ~0ull;
-    s.entries([&](int token, float v) {
-      if (v == m) first = Min::two(first, static_cast<u64>(token));
-    });
+    const auto look = [&](int token, const uint4& r) {
+#pragma unroll
+      for (int e = 0; e < Elem<DT>::E; ++e)
+        if (entry<DT>(r, e) == m) first = Min::two(first, static_cast<u64>(token + e));
+    };
+    if constexpr (kStream)
+      in_groups<DT>(h, s, p.c, of_groups, m, look);
+    else if (own == m)
+      s.raw(look);
     const int token = static_cast<int>(exchange<Min>(x, w.turn, parts, rank, first).a);
     if (rank == 0 && tid == 0) {
       p.tokens[row] = token;
@@ -889,7 +896,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
       unsigned unused = 0;
       if (!by_k) sum = weight.of_all(s, unused);
       if (kStream && by_k) {
-        list_groups<DT>(h, s, p.c, of_groups, from);
+        in_groups<DT>(h, s, p.c, of_groups, from, [&](int token, const uint4& r) { list_from<DT>(h, from, token, r); });
       } else if (own >= from) {
         s.raw([&](int token, const uint4& r) {
           const unsigned in = list_from<DT>(h, from, token, r);
@@ -1118,7 +1125,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_top_kernel(const TopPara
   if (p.k <= kHeadMost) {
     const float from = reached_by(h, groups, own, p.k);
     if constexpr (kStream) {
-list_groups<DT>(h, s, p.c, own, from);
+      in_groups<DT>(h, s, p.c, own, from, [&](int token, const uint4& r) { list_from<DT>(h, from, token, r); });
     } else if (mine >= from) {
       s.raw([&](int token, const uint4& r) { list_from<DT>(h, from, token, r); });
     }
@@ -1200,9 +1207,14 @@ cos_status check_rows(const void* logits, long long stride, int rows, int vocab,
   return COS_OK;
 }
 
-// A block for each row where there are rows enough and one does not fit into a block's shared memory (top 64 of 64 rows of 128256 bf16 13.0 us, on clusters 14.0; of 256 19.9 and 47;
-// of 32 12.7 and 10.2; of 256 rows of 8000 12.7 and 7.3).
-bool own_blocks(int rows, int vocab, int dtype) { return rows >= 48 && static_cast<long long>(vocab) * (dtype == COS_DTYPE_F32 ? 4 : 2) > kMostKept; }
+// A block for each row where there are rows enough, and too long for a block's shared memory: no exchanges, and one wave where clusters take several.  Rows from which on (us, clusters / a block
+// a row, logits drawn from N(0, 2.5^2)):
+//   top logits, k <= 64     48   64 of 48 x 128256 bf16 13.5 / 13.2, of 32 rows 9.9 / 12.7, of 100 21.0 / 13.0
+//   top logits, more        80   288 of 80 x 256000 bf16 42.6 / 32.6, of 64 rows 32.5 / 32.4, of 64 x 128256 23.4 / 28.6 (their groups are read again in turns)
+//   a draw, k <= 64         16   64 of 16 x 128256 bf16 11.5 / 11.0, of 8 x 256000 (k = 50) 11.8 / 12.1, of 100 x 128256 26.5 / 11.7
+//   a draw, more            40   200 of 40 x 128256 bf16 22.3 / 20.2, of 32 rows 19.7 / 20.7, of 100 33.9 / 20.9
+//   the largest logit       16   16 x 128256 bf16 5.0 / 4.6, 100 rows 13.2 / 4.8, 64 x 32000 4.7 / 3.3; not for shorter rows (256 x 16000 4.2 / 5.2)
+bool own_blocks(int rows, int vocab, int dtype, int from, int longer_than = kMostKept) { return rows >= from && static_cast<long long>(vocab) * (dtype == COS_DTYPE_F32 ? 4 : 2) > longer_than; }
 
 template <class P, class F>
 cos_status launch_rows(P& p, int rows, int vocab, int dtype, int device, size_t shared, bool whole, cudaStream_t stream, F&& kernel_of) {
@@ -1295,9 +1307,11 @@ extern "C" cos_status cos_sample(const cos_sample_args* a, void* cuda_stream) {
       return dt == COS_DTYPE_F32 ? cos_sample_kernel<COS_DTYPE_F32, kStream> : (dt == COS_DTYPE_BF16 ? cos_sample_kernel<COS_DTYPE_BF16, kStream> : cos_sample_kernel<COS_DTYPE_F16, kStream>);
     });
   };
-  // A block for each row as for top logits, where the host knows that the rows are done with their heads.
-  const bool head = !a->row_top_k && !a->row_temperature && a->temperature > 0.0f && a->top_k > 0 && a->top_k <= kHeadMost && a->top_k < a->vocab;
-  return head && own_blocks(a->rows, a->vocab, a->dtype) ? call(std::true_type()) : call(std::false_type());
+  // A block for each row where the host knows that the rows are done with their heads or maxima.
+  const bool largest = !a->row_temperature && a->temperature == 0.0f;
+  const bool head = !a->row_temperature && !largest && !a->row_top_k && a->top_k > 0 && a->top_k <= kHeadMost && a->top_k < a->vocab;
+  const bool own = (largest && own_blocks(a->rows, a->vocab, a->dtype, 16, kMostKept / 2)) || (head && own_blocks(a->rows, a->vocab, a->dtype, a->top_k <= 64 ? 16 : 40));
+  return own ? call(std::true_type()) : call(std::false_type());
 }
 
 extern "C" cos_status cos_top_logits(const cos_top_args* a, void* cuda_stream) {
@@ -1326,5 +1340,5 @@ extern "C" cos_status cos_top_logits(const cos_top_args* a, void* cuda_stream) {
   };
   using Few = std::integral_constant<int, kCandidates>;
   if (a->k > kMost<kCandidates>) return call(std::integral_constant<int, kTopCandidates>(), std::false_type());
-  return own_blocks(a->rows, a->vocab, a->dtype) ? call(Few(), std::true_type()) : call(Few(), std::false_type());
+  return own_blocks(a->rows, a->vocab, a->dtype, a->k <= 64 ? 48 : 80) ? call(Few(), std::true_type()) : call(Few(), std::false_type());
 }

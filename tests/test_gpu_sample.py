@@ -283,3 +283,30 @@ def test_many_long_rows(dtype):
     got = pkg.sample(x, u, 0.8, 60, 0.95, 0.01, filtered=x)
     assert torch.equal(torch.nan_to_num(x.float(), nan=-7.0), torch.nan_to_num(want["filtered"].float(), nan=-7.0)) and torch.equal(got["tokens"], want["tokens"])
     assert torch.equal(x.as_strided((rows, 1), (V + 1, 1), V), kept)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,V", [(15, 40001), (17, 20001), (39, 40001)])
+def test_few_long_rows(rows, V, dtype):
+    """Either side of the numbers of rows from which on a row has a block: the largest logit and a few, ties and masks among them, in place."""
+    x, u = make(rows, V, dtype, seed=rows, pad=3)
+    inf = float("inf")
+    x[1] = -2.0
+    x[2] = -inf
+    x[3, : V - 1] = -inf
+    x[4, 9] = float("nan")
+    x[5, 11] = inf
+    x[6] = torch.finfo(x.dtype).min
+    x[7, 100::1000] = 60.0
+    x[8, V - 1] = 60.0
+    x[9, 0] = 60.0
+    x[10, 1::2] = -inf
+    for T, k, p, least in ((0.0, 0, 1.0, 0.0), (0.0, 20, 0.3, 0.9), (0.8, 64, 0.9, 0.0), (0.8, 65, 1.0, 0.01)):
+        run(x, u, T, k, p, least)
+    for T, k in ((0.0, 0), (0.8, 64)):
+        y = x.as_strided((rows, V + 3), (V + 3, 1), 0).clone()
+        rest = y[:, V:].clone()
+        want = run(x, u, T, k)
+        got = pkg.sample(y[:, :V], u, T, k, filtered=y[:, :V])
+        assert torch.equal(torch.nan_to_num(y[:, :V].float(), nan=-7.0), torch.nan_to_num(want["filtered"].float(), nan=-7.0)) and torch.equal(got["tokens"], want["tokens"])
+        assert torch.equal(y[:, V:], rest)

@@ -131,3 +131,22 @@ def test_many_rows(dtype):
     x[11, ::2] = -float("inf")
     for k in (1, 64, 288, 1000):
         check(x, k, 1.0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows", [47, 49, 81])
+def test_long_rows(rows, dtype):
+    """Either side of the numbers of rows from which on a row has a block."""
+    V, inf = 40003, float("inf")
+    g = torch.Generator("cuda").manual_seed(rows)
+    x = (2.5 * torch.randn((rows, V), generator=g, device="cuda")).to(DTYPES[dtype])
+    x[1] = 0.5
+    x[2] = -inf
+    x[3, 10:] = -inf
+    x[4, 5] = float("nan")
+    x[5, 7] = inf
+    x[6, 1:] = torch.finfo(x.dtype).min
+    x[7] = torch.randint(0, 3, (V,), generator=g, device="cuda").to(x.dtype)
+    x[8, ::2] = -inf
+    for k in (1, 64, 65, 288, 289):
+        check(x, k, 0.7)

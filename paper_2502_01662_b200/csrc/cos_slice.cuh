@@ -120,6 +120,8 @@ struct RowSlice {
     kept = smem;
     res = res_;
   }
+  // the warp that has a token of the slice
+  __device__ __forceinline__ int warp_of(int token, int seg) const { return static_cast<int>((static_cast<long long>(token) + off) / E - v0) / seg; }
   // the token of a vector's first entry (negative where the row starts inside it)
   __device__ __forceinline__ int token(int i) const { return static_cast<int>(static_cast<long long>(v0 + i) * E - off); }
   __device__ __forceinline__ uint4 fetch(int i) const {

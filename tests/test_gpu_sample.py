@@ -310,3 +310,16 @@ def test_few_long_rows(rows, V, dtype):
         got = pkg.sample(y[:, :V], u, T, k, filtered=y[:, :V])
         assert torch.equal(torch.nan_to_num(y[:, :V].float(), nan=-7.0), torch.nan_to_num(want["filtered"].float(), nan=-7.0)) and torch.equal(got["tokens"], want["tokens"])
         assert torch.equal(y[:, V:], rest)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,V", [(1, 3001), (300, 3001), (3, 16001), (2, 131071), (40, 131071)])
+def test_limits_far_down_the_line(rows, V, dtype):
+    """Flat rows, whose limit by mass lies behind thousands of tokens: uniforms all over the mass, ties at the limit, min-p before and behind it."""
+    g = torch.Generator("cuda").manual_seed(rows + V)
+    x = (1.5 * torch.rand((rows, V), generator=g, device="cuda")).to(DTYPES[dtype])
+    x[0, : V // 2] = 0.75  # (a limit among equals, of more than a list holds)
+    x[rows // 2, ::3] = -float("inf")
+    u = (torch.arange(rows, device="cuda") + 0.5) / rows
+    for T, k, p, least in ((1.0, 0, 0.5, 0.0), (0.3, 0, 0.9, 0.0), (1.0, 2 * V // 3, 0.6, 0.0), (1.0, 0, 0.7, 0.5), (0.7, 0, 0.2, 0.01), (1.0, 2000, 0.9999, 0.0)):
+        run(x, u, T, k, p, least)

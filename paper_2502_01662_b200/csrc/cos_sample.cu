@@ -957,8 +957,9 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
     }
     // Bins of 1/64 of a logit for a top-k alone, of 1/32 of a power of two of the weight for both (twice that where there are 512).  For a top-p alone they reach as far as its limit may lie: all logits
     // whose weight is below (1 - p) / vocab of the total have less than (1 - p) of it together, and are left out.
-    // 512 bins over 16 blocks, whose bins take 7000 clocks to read otherwise.
-    const int bins = parts > 8 ? kBins / 2 : kBins;
+    // 512 bins over 16 blocks, whose bins take 7000 clocks to read otherwise; not for rows so long that the limit's bin would then hold more than the list does (256000 of N(0, 2.5^2) at p = 0.9:
+    // some rows 56 us).
+    const int bins = parts > 8 && p.c.V <= 320 * kCandidates ? kBins / 2 : kBins;
     bool cut = false;
     float per_unit = static_cast<float>(bins / 32);
     if (by_p && !by_k) {
@@ -1279,9 +1280,14 @@ cudaError_t slice_plan(int device, int rows, int vocab, int dtype, int most, boo
   const long long all = (static_cast<long long>(vocab) + 2 * (E - 1)) / E;
   long long parts = 1;
   while ((parts < kSliceParts || !cluster) && (all + parts - 1) / parts > kept) parts *= 2;
-  const long long places[5] = {0, 2 * plan->sms, 2 * plan->sms, 256, 192};  // for blocks of rows in 1, 2, 4, 8, 16
-  for (int two = 1; two <= 4; ++two)
-    if (parts == 1ll << (two - 1) && all / parts >= kSliceThreads && rows * parts * 2 <= places[two]) parts *= 2;
+  // Places for blocks of rows in 2, 4, 8, 16.  Blocks in eights and sixteens that share a multiprocessor pay where slices are long only (us, of 12 rows in eights / sixteens: top 256 of 32000 fp32
+  // 7.2 / 8.7, p = 0.9 18.7 / 21.9, drawn from 256000 bf16 18.2 / 14.7; of 24 rows in fours / eights: k = 50 of 32000 bf16 8.6 / 10.4, drawn from 128256 bf16 18.3 / 15.3).
+  const auto places = [&](long long blocks) -> long long {
+    const bool longer = all / (blocks / 2) * 16 > (blocks == 8 ? 24 : 48) * 1024;
+    return blocks < 8 ? 2 * plan->sms : blocks == 8 ? (longer ? 256 : 120) : (longer ? 192 : 112);
+  };
+  for (long long blocks = 2; blocks <= kSliceParts; blocks *= 2)
+    if (parts == blocks / 2 && all / parts >= kSliceThreads && rows * blocks <= places(blocks)) parts = blocks;
   plan->parts = static_cast<int>(parts);
   plan->share = static_cast<int>((all + parts - 1) / parts);
   plan->seg = static_cast<int>((plan->share + 32 * kSliceWarps - 1) / (32 * kSliceWarps) * 32);

@@ -366,7 +366,7 @@ __device__ __forceinline__ Words exchange(Exchange& x, int& turn, int parts, int
 
 // How a row is cut up: as few blocks as `most` bytes of shared memory each allow (16 at most: what does not fit is read again where it is wanted), or more where
 // all of them still have their places side by side (two a multiprocessor; of clusters of 8 and 16 there are places for 32 and 12 or so, since one lies in a
-// group of 16 to 20 multiprocessors), down to a vector a thread.  cluster: the blocks are one (a power of two).
+// group of 16 to 20 multiprocessors, and for 15 and 7 with a multiprocessor for each block), down to a vector a thread.  cluster: the blocks are one (a power of two).
 struct SlicePlan {
   int parts, share, seg, res, sms;
   size_t smem;

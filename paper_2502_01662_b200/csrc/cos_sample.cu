@@ -4,7 +4,7 @@
 // Mathematics.  In order of (logit down, index up) every one of the three limits keeps a beginning of the line, so what is kept is the tokens at or
 // above one of them.  A token's place in the line is one 64-bit number (`place_of`).
 //
-// The head of the line is found without sorting or counting tokens: of 512 groups of tokens (the same for all blocks) each block gets the largest logit; the
+// The head of the line is found without sorting or counting tokens: of 512 groups of tokens (the same for all blocks; 1024 where a block has the row for itself) each block gets the largest logit; the
 // k-th largest of these is at most the k-th largest logit, and little below it (k of 512 groups are taken up by some -512 ln(1 - k/512) tokens: 53 for k = 50).
 // The few tokens from there on are compared with one another, and where the limits lie among them the row is done (top-k up to kHeadMost; top-p whose tokens
 // are among the first few hundred).  Else a histogram of 1024 bins, linear in the logit below the maximum, says in which bin a limit lies, and the places in
@@ -15,6 +15,10 @@
 // series of 2^r for |r| <= 2^-10 (the fourth term is below 1e-14), rounded to whole multiples of 2^-scale and summed as integers: a token is drawn where a
 // border of the cumulative sums lies next to u, and 32-bit sums are off by more than the weight of a token there.  Integers make sums independent of their
 // order, so atomics and the split over blocks change nothing.
+//
+// Bound by latency, not bytes: a draw from one row of 151936 bf16 under top-k and top-p takes 8.7 us, three exchanges over 16 blocks (1.3 us each) among them; 64 x 256000 bf16 drawn from
+// whole 33 us (1 TB/s; two waves of clusters, issue slots half busy); 32 x 128256 bf16 with a flat nucleus among them 42 us, the time of
+// the rows that take the general path.  A block for each row, in registers: top 64 of 512 x 128256 bf16 38.5 us, 3.4 TB/s, 20 us at the copy rate (four rows on some multiprocessors, three on others).
 #include <float.h>
 
 #include "cos_slice.cuh"

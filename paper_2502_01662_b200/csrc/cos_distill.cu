@@ -23,6 +23,7 @@ struct Statistics {
   double listed, mass64;
 };
 static_assert(sizeof(Statistics) == COS_DISTILL_STATISTICS * sizeof(float), "as the header says");
+constexpr int kMostKept = 64 * 1024;  // bytes of a slice: three blocks of a multiprocessor have room for that
 constexpr int kLoss = 0, kGrad = 1, kStep = 2, kShareThreads = 128;
 
 struct DistillParams {
@@ -436,7 +437,7 @@ cos_status distill(const cos_distill_args* a, void* cuda_stream) {
   OnDevice on(a->device);
   if (on.error != cudaSuccess) return call_failed("cudaSetDevice", on.error);
   SlicePlan plan;
-  cudaError_t e = slice_plan(a->device, a->rows, a->vocab, a->dtype, 64 * 1024, MODE != kGrad, &plan);
+  cudaError_t e = slice_plan(a->device, a->rows, a->vocab, a->dtype, kMostKept, MODE != kGrad, &plan);
   if (e != cudaSuccess) return call_failed("device query", e);
   if (static_cast<long long>(a->rows) * plan.parts > 0x7fffffffll) return call_failed(COS_ERR_UNSUPPORTED, "too many rows for one launch");
   DistillParams p = {};
@@ -473,12 +474,13 @@ cos_status distill(const cos_distill_args* a, void* cuda_stream) {
     constexpr int DT = decltype(dt)::value;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (MODE != kGrad) {
-      const cudaError_t first = slice_launch(cos_distill_shares_kernel<DT>, p, a->rows, 1, static_cast<size_t>(a->lists) * a->k * (sizeof(double) + sizeof(int) + sizeof(float)), stream, kShareThreads);
+      constexpr size_t entry = sizeof(double) + sizeof(int) + sizeof(float);
+      const cudaError_t first = slice_launch(cos_distill_shares_kernel<DT>, p, a->rows, 1, static_cast<size_t>(a->lists) * a->k * entry, COS_TOP_MAX * entry, stream, kShareThreads);
       if (first != cudaSuccess) return first;
     }
-    if (stream_warps == 8) return slice_launch(cos_distill_stream_kernel<DT, 8>, p, a->rows, 1, 0, stream, 256);
-    if (stream_warps == 16) return slice_launch(cos_distill_stream_kernel<DT, 16>, p, a->rows, 1, 0, stream, 512);
-    return slice_launch(cos_distill_kernel<DT, MODE>, p, a->rows * plan.parts, MODE == kGrad ? 1 : plan.parts, plan.smem, stream);
+    if (stream_warps == 8) return slice_launch(cos_distill_stream_kernel<DT, 8>, p, a->rows, 1, 0, 0, stream, 256);
+    if (stream_warps == 16) return slice_launch(cos_distill_stream_kernel<DT, 16>, p, a->rows, 1, 0, 0, stream, 512);
+    return slice_launch(cos_distill_kernel<DT, MODE>, p, a->rows * plan.parts, MODE == kGrad ? 1 : plan.parts, plan.smem, kMostKept, stream);
   };
   e = a->dtype == COS_DTYPE_F32    ? launches(std::integral_constant<int, COS_DTYPE_F32>())
       : a->dtype == COS_DTYPE_BF16 ? launches(std::integral_constant<int, COS_DTYPE_BF16>())

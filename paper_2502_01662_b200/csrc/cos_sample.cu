@@ -1269,7 +1269,7 @@ cos_status launch_rows(P& p, int rows, int vocab, int dtype, int device, size_t 
   p.c.share = plan.share;
   p.c.seg = plan.seg;
   p.c.res = plan.res;
-  e = slice_launch(kernel_of(dtype), p, rows * plan.parts, plan.parts, shared + plan.smem, stream);
+  e = slice_launch(kernel_of(dtype), p, rows * plan.parts, plan.parts, shared + plan.smem, shared + kMostKept, stream);
   return e == cudaSuccess ? COS_OK : call_failed("launch", e);
 }
 

@@ -397,9 +397,10 @@ struct OnDevice {
   }
 };
 
+// most: of shared memory, that the kernel is ever launched with (the attribute is the kernel's, and calls of other threads may come between it and the launch: they all set the same)
 template <class P>
-cudaError_t slice_launch(void (*fn)(P), const P& p, int blocks, int parts, size_t smem, cudaStream_t stream, int threads = kSliceThreads) {
-  cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+cudaError_t slice_launch(void (*fn)(P), const P& p, int blocks, int parts, size_t smem, size_t most, cudaStream_t stream, int threads = kSliceThreads) {
+  cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(most));
   if (e == cudaSuccess && parts > 8) e = cudaFuncSetAttribute(fn, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t lc = {};

@@ -108,3 +108,32 @@ def test_the_same_complaints(monkeypatch):
             with pytest.raises(error):
                 call()
         both(monkeypatch, check)
+
+
+def test_calls_of_several_threads():
+    """Calls at once whose launches take different amounts of shared memory: none fails, all results are those of calls one by one."""
+    import threading
+    sizes = [(2, 900), (3, 60000), (40, 32000), (5, 9000)]
+    rows = [(torch.randn(n, V, device="cuda", generator=torch.Generator("cuda").manual_seed(V)), torch.rand(n, device="cuda")) for n, V in sizes]
+    def calls(x, u):
+        top = pkg.top_logits(x, 20)
+        step = pkg.distill_step(x, top["ids"], top["values"] + 0.1, u, top["lse"])
+        return pkg.sample(x, u, 0.9, 0, 0.9)["tokens"], top["ids"], step["grad"], step["loss"]
+    want = [calls(x, u) for x, u in rows]
+    wrong = []
+    def work(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(100):
+                    got = calls(*rows[i])
+                    if not all(torch.equal(a, b) for a, b in zip(got, want[i])):
+                        wrong.append(i)
+        except Exception as e:  # noqa: BLE001
+            wrong.append(e)
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(rows))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong, wrong[:3]

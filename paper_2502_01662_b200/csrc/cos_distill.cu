@@ -428,7 +428,7 @@ cos_status distill(const cos_distill_args* a, void* cuda_stream) {
     if (!a->row_weights || !a->grad) return call_failed(COS_ERR_INVALID_ARG, "null device pointer");
     if (misaligned(a->grad, bytes)) return call_failed(COS_ERR_ALIGNMENT, "grad pointer not aligned to its element type");
     if (a->rows > 1 && a->stride_grad < a->vocab) return call_failed(COS_ERR_INVALID_ARG, "rows overlap: stride_grad is less than vocab");
-    if (a->grad == a->student && a->rows > 1 && a->stride_grad != a->stride_student) return call_failed(COS_ERR_INVALID_ARG, "a gradient in place needs the stride of the student");
+    if (overlap(a->student, a->stride_student, a->grad, a->stride_grad, a->rows, a->vocab, bytes)) return call_failed(COS_ERR_INVALID_ARG, "grad overlaps the student (in place: the same address and stride)");
   }
   if (misaligned(a->ids, 4) || misaligned(a->values, 4) || misaligned(a->lse, 4) || (MODE != kGrad && misaligned(a->loss, 4)) || (MODE != kLoss && misaligned(a->row_weights, 4)))
     return call_failed(COS_ERR_ALIGNMENT, "an int32/float pointer is not 4-byte aligned");

@@ -1319,7 +1319,8 @@ extern "C" cos_status cos_sample(const cos_sample_args* a, void* cuda_stream) {
   if (a->filtered) {
     if (reinterpret_cast<uintptr_t>(a->filtered) % (a->dtype == COS_DTYPE_F32 ? 4 : 2)) return call_failed(COS_ERR_ALIGNMENT, "filtered pointer not aligned to its element type");
     if (a->rows > 1 && a->stride_filtered < a->vocab) return call_failed(COS_ERR_INVALID_ARG, "rows overlap: stride_filtered is less than vocab");
-    if (a->filtered == a->logits && a->rows > 1 && a->stride_filtered != a->stride_row) return call_failed(COS_ERR_INVALID_ARG, "filtered in place needs the stride of the logits");
+    if (overlap(a->logits, a->stride_row, a->filtered, a->stride_filtered, a->rows, a->vocab, a->dtype == COS_DTYPE_F32 ? 4 : 2))
+      return call_failed(COS_ERR_INVALID_ARG, "filtered overlaps the logits (in place: the same address and stride)");
   }
   SampleParams p = {};
   p.c.logits = a->logits;

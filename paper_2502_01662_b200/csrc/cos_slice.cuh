@@ -383,6 +383,17 @@ cudaError_t slice_plan(int device, int rows, int vocab, int dtype, int most, boo
 cos_status call_failed(cos_status st, const char* what);
 cos_status call_failed(const char* what, cudaError_t e);
 
+// Whether rows that a call writes share an entry with rows that it reads, other than being the same ones (strides in entries of `bytes`; in: 0 for one row for all).
+inline bool overlap(const void* in, long long stride_in, const void* out, long long stride_out, int rows, int vocab, int bytes) {
+  const long long row = static_cast<long long>(vocab) * bytes, a = reinterpret_cast<long long>(in), b = reinterpret_cast<long long>(out), sa = stride_in * bytes, sb = stride_out * bytes;
+  if (a == b) return rows > 1 && sa != sb;
+  if (rows == 1) return a < b + row && b < a + row;
+  if (b >= a + (rows - 1) * sa + row || a >= b + (rows - 1) * sb + row) return false;
+  if (sa != sb) return true;
+  const long long apart = ((b - a) % sa + sa) % sa;  // columns of one buffer
+  return apart < row || apart > sa - row;
+}
+
 // The device of a call, made current for its duration.
 struct OnDevice {
   int before = -1;

@@ -127,3 +127,19 @@ def test_the_binding_refuses():
                  lambda: pkg.distill_loss(x, ids, values, temperature=0.0), lambda: pkg.distill_loss(x, ids, values, weights=[-1.0])):
         with pytest.raises(pkg.CosVerifyError):
             call()
+
+
+@pytest.mark.parametrize("rows,stride,out,stride_out,refused", [
+    (1, 100, 99, 100, True), (1, 100, 100, 100, False), (1, 100, -100, 100, False), (1, 100, -99, 100, True), (4, 100, 100, 100, True), (4, 100, 400, 100, False), (4, 100, -400, 100, False),
+    (4, 100, -399, 100, True), (4, 220, 100, 220, False), (4, 220, 120, 220, False), (4, 220, 121, 220, True), (4, 220, 99, 220, True), (4, 220, -100, 220, False), (4, 220, -121, 220, True),
+    (4, 220, 540, 220, False), (4, 220, 100, 221, True), (4, 0, 50, 100, True), (4, 0, 100, 100, False), (4, 0, -300, 100, True), (4, 0, -400, 100, False)])
+def test_outputs_that_overlap_inputs(rows, stride, out, stride_out, refused):
+    """Columns of one buffer are apart or not by their distance in a row; what is refused is refused by reason of that, the others for a device that is not there."""
+    for (fn, a, _), of in ((_sample(), "filtered"), (_distill("cos_distill_grad"), "grad"), (_distill("cos_distill_step"), "grad")):
+        size = 4 if a.dtype == 0 else 2
+        a.rows, a.device = rows, 1 << 20
+        setattr(a, "stride_row" if of == "filtered" else "stride_student", stride)
+        setattr(a, of, A + out * size)
+        setattr(a, "stride_" + of, stride_out)
+        st = fn(ctypes.byref(a), None)
+        assert (st == 1) == refused and st != 0 and (b"overlaps" in pkg.load_library().cos_verify_last_error(None)) == refused

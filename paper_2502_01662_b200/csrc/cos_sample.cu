@@ -884,8 +884,8 @@ __global__ void __launch_bounds__(kSliceThreads, 2) cos_sample_kernel(const Samp
   Weight<DT> weight;
   weight.init(m, T, p.c.V, table);
   const auto weigh = [&](float v) { return weight.of(v); };
-  // min-p as a logit: w >= min_p where l >= m + T ln(min_p)
-  const float least = min_p > 0.0f ? __double2float_ru(fma(static_cast<double>(T), log(fmin(static_cast<double>(min_p), 1.0)), static_cast<double>(m))) : -INFINITY;
+  // min-p as a logit: w >= min_p where l >= m + T ln(min_p); at a T without an end every token weighs 1
+  const float least = min_p > 0.0f && T < INFINITY ? __double2float_ru(fma(static_cast<double>(T), log(fmin(static_cast<double>(min_p), 1.0)), static_cast<double>(m))) : -INFINITY;
   const auto share_of = [&](u64 mass) {  // of top-p: at least a unit, so that the first token is kept
     const double want = ceil(static_cast<double>(fmaxf(top_p, 0.0f)) * static_cast<double>(mass));
     return want < 1.0 ? 1ull : static_cast<u64>(want);

@@ -323,3 +323,22 @@ def test_limits_far_down_the_line(rows, V, dtype):
     u = (torch.arange(rows, device="cuda") + 0.5) / rows
     for T, k, p, least in ((1.0, 0, 0.5, 0.0), (0.3, 0, 0.9, 0.0), (1.0, 2 * V // 3, 0.6, 0.0), (1.0, 0, 0.7, 0.5), (0.7, 0, 0.2, 0.01), (1.0, 2000, 0.9999, 0.0)):
         run(x, u, T, k, p, least)
+
+
+@pytest.mark.parametrize("k,p,least", [(0, 1.0, 1.0), (0, 1.0, 0.5), (20, 1.0, 1.0), (20, 0.4, 1.0), (0, 0.01, 1.0), (300, 0.9, 0.0)])
+def test_a_temperature_without_an_end(k, p, least):
+    """Every token weighs the same, and min-p takes none."""
+    x, u = make(50, 2000, "f32", seed=5)
+    x[1, ::2] = -float("inf")
+    out = pkg.sample(x, u, float("inf"), k, p, least)
+    for n in range(50):
+        row = x[n].cpu().numpy().astype(np.float64)
+        line = np.argsort(-row, kind="stable")[: int(np.isfinite(row).sum())]
+        line = line[: k] if k else line
+        total = len(line)
+        line = np.sort(line[: int(np.ceil(np.float64(np.float32(p)) * total))])
+        assert int(out["kept"][n]) == len(line) and int(out["row_status"][n]) == 0
+        at = np.float64(np.float32(u[n].item())) * len(line)
+        assert abs(at - round(at)) > 1e-6  # (no uniform lies on a border)
+        assert int(out["tokens"][n]) == line[int(np.floor(at))]
+        assert abs(float(out["prob"][n]) - 1.0 / len(line)) <= 2.0 ** -24 / len(line)

@@ -6,6 +6,7 @@ proposer from such lists.  Argument marshalling only, as in `binding`: the arith
 from __future__ import annotations
 
 import ctypes
+import operator
 from typing import Optional, Sequence
 
 from .binding import COS_MAX_MODELS, COS_OK, CosVerifyError, _current_stream, _dtype_code, load_call, load_library
@@ -84,6 +85,8 @@ def _rows(t, name: str):
     rows, vocab = t.shape
     if rows < 1 or vocab < 1:
         raise ValueError(f"{name} must have at least one row and one entry")
+    if max(rows, vocab) > 2 ** 31 - 1:
+        raise ValueError(f"{name} has more rows or entries than 32 bits count")
     if vocab > 1 and t.stride(1) != 1:
         raise ValueError(f"the vocabulary axis of {name} must be contiguous")
     return rows, vocab, t.stride(0) if rows > 1 else vocab
@@ -137,7 +140,7 @@ def sample(logits, uniforms, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, fil
         if isinstance(v, torch.Tensor):
             setattr(a, "row_" + name, _small(v, name, (rows,), dtype, device))
         else:
-            setattr(a, name, v)
+            setattr(a, name, v if name != "top_k" else max(-1, min(operator.index(v), 2 ** 31 - 1)))     # (a vocabulary has no more)
     buf = torch.empty((4, rows), dtype=torch.int32, device=device)
     tokens, kept, status, prob = buf.unbind(0)
     out = {"tokens": tokens, "prob": prob.view(torch.float32), "kept": kept, "row_status": status}

@@ -137,3 +137,16 @@ def test_calls_of_several_threads():
     for t in threads:
         t.join()
     assert not wrong, wrong[:3]
+
+
+@pytest.mark.parametrize("k", [2 ** 31 - 1, 2 ** 31, 2 ** 32 + 5, 2 ** 70, -(2 ** 31), -(2 ** 32) + 5])
+def test_numbers_beyond_32_bits_are_no_limit(k):
+    x, u = torch.randn(3, 500, device="cuda"), torch.rand(3, device="cuda")
+    want, got = pkg.sample(x, u), pkg.sample(x, u, top_k=k)
+    assert all(torch.equal(got[n], want[n]) for n in want) and (got["kept"] == 500).all()
+
+
+def test_more_rows_than_32_bits():
+    x = torch.zeros((1, 4), device="cuda").expand(2 ** 31, 4)
+    with pytest.raises(ValueError):
+        pkg.top_logits(x, 2)

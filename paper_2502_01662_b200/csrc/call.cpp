@@ -8,11 +8,13 @@
 #include <ATen/ops/as_strided.h>
 #include <ATen/ops/empty.h>
 #include <Python.h>
+#include <c10/cuda/CUDAGraphsC10Utils.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/autograd/variable.h>
 
 #include <new>
 #include <optional>
@@ -349,6 +351,14 @@ bool distill_of(PyObject* const* a, cos_distill_args* v, const at::Tensor** stud
 at::Tensor floats(const at::Tensor& like, int64_t n) { return at::empty({n}, like.options().dtype(at::kFloat).requires_grad(false)); }
 int64_t statistics_size(const cos_distill_args& v) { return static_cast<int64_t>(v.rows) * (COS_DISTILL_STATISTICS + v.lists * v.k); }
 
+// A leaf whose gradient is taken up on the default stream (an eager graph of it is alive) has no backward pass in a capture: the engine would wait for that stream there, whose error nobody catches.
+void refuse_capture(const at::Tensor& student) {
+  if (!student.requires_grad() || !student.is_leaf() || c10::cuda::currentStreamCaptureStatusMayInitCtx() == c10::cuda::CaptureStatus::None) return;
+  const auto takes = torch::autograd::impl::try_get_grad_accumulator(student);
+  const auto on = takes ? takes->stream() : std::nullopt;
+  TORCH_CHECK(!on || on->id() != 0, "distill_loss: a backward pass of this leaf cannot be captured while an eager graph of it is alive");
+}
+
 // The loss as a node of the autograd graph.  `grad_fn` is cos_distill_grad; `st` takes the status of the forward call.
 struct DistillLoss : torch::autograd::Function<DistillLoss> {
   static at::Tensor forward(torch::autograd::AutogradContext* ctx, const at::Tensor& student, const at::Tensor& ids, const at::Tensor& values, const std::optional<at::Tensor>& lse, const cos_distill_args* args,
@@ -371,6 +381,7 @@ struct DistillLoss : torch::autograd::Function<DistillLoss> {
     const auto saved = ctx->get_saved_variables();
     const auto numbers = ctx->saved_data["numbers"].toDoubleVector();
     const at::Tensor& student = saved[0];
+    refuse_capture(student);
     at::Tensor grad;
     {
       const at::AutoGradMode off(false);

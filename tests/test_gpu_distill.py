@@ -287,3 +287,35 @@ def test_many_rows(dtype):
     s[6, 9] = float("inf")
     loss = pkg.distill_loss(s, ids, values, lse, [0.5, 0.5])
     assert loss[4:7].isnan().all() and loss[:4].isfinite().all() and loss[7:].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_captured_backward_pass(dtype):
+    """Forward and backward in a graph, replayed on other inputs; while an eager graph of the same leaf is alive the backward pass is refused, and the process goes on."""
+    s, ids, values, lse = make(7, 3001, dtype, 1, 16, seed=21)
+    rw = torch.rand(7, device="cuda")
+    static = s.clone().requires_grad_(True)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        loss = pkg.distill_loss(static, ids, values, lse)
+        grad, = torch.autograd.grad(loss, static, rw)
+    for turn in range(2):
+        with torch.no_grad():
+            static.copy_(s.roll(turn, 0))
+        graph.replay()
+        leaf = s.roll(turn, 0).requires_grad_(True)
+        want = pkg.distill_loss(leaf, ids, values, lse)
+        assert torch.equal(loss, want) and torch.equal(grad, torch.autograd.grad(want, leaf, rw)[0])
+    leaf = s.clone().requires_grad_(True)
+    alive = pkg.distill_loss(leaf, ids, values, lse)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        inside = pkg.distill_loss(leaf, ids, values, lse)
+        with pytest.raises(RuntimeError, match="eager graph"):
+            torch.autograd.grad(inside, leaf, rw)
+    graph.replay()
+    assert torch.equal(inside, alive)
+    again, = torch.autograd.grad(alive, leaf, rw)
+    assert torch.equal(again, torch.autograd.grad(pkg.distill_loss(leaf, ids, values, lse), leaf, rw)[0])

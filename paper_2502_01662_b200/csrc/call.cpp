@@ -51,6 +51,15 @@ PyObject* callee(PyObject*, PyObject* args) {
   return capsule;
 }
 
+// Without the interpreter's lock until the end of the scope, however that is left: what throws there (an allocation, a hook on saved tensors) becomes a Python error, which needs the lock.
+struct Unlocked {
+  PyThreadState* const state = PyEval_SaveThread();
+  Unlocked() = default;
+  Unlocked(const Unlocked&) = delete;
+  Unlocked& operator=(const Unlocked&) = delete;
+  ~Unlocked() { PyEval_RestoreThread(state); }
+};
+
 // A plain int32 device tensor that is contiguous, with anything in it.
 bool plain_int32(PyObject* o) {
   if (!THPVariable_CheckExact(o)) return false;
@@ -132,9 +141,10 @@ PyObject* run(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     v.out_tokens = at0 + 3 * B;
     void* stream = c10::cuda::getCurrentCUDAStream(logits.get_device()).stream();
     cos_status st;
-    Py_BEGIN_ALLOW_THREADS
-    st = c->run(c->ctx, &v, stream);
-    Py_END_ALLOW_THREADS
+    {
+      const Unlocked unlocked;
+      st = c->run(c->ctx, &v, stream);
+    }
     if (st != COS_OK) return PyLong_FromLong(st);
     const at::Tensor outs[4] = {at::as_strided(buf, {B}, {1}, 0), at::as_strided(buf, {B, P}, {P, 1}, 3 * B), at::as_strided(buf, {B}, {1}, B),
                                 at::as_strided(buf, {B}, {1}, 2 * B).view(at::kFloat)};
@@ -269,9 +279,10 @@ PyObject* sample(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     v.row_status = reinterpret_cast<uint32_t*>(at0 + 2 * rows);
     v.prob = reinterpret_cast<float*>(at0 + 3 * rows);
     cos_status st;
-    Py_BEGIN_ALLOW_THREADS
-    st = enqueue(fn, v, logits->device().index());
-    Py_END_ALLOW_THREADS
+    {
+      const Unlocked unlocked;
+      st = enqueue(fn, v, logits->device().index());
+    }
     if (st != COS_OK) return PyLong_FromLong(st);
     const auto part = [&](int64_t i) { return at::as_strided(buf, {rows}, {1}, i * rows); };
     return dict_of({{"tokens", part(0)}, {"prob", part(3).view(at::kFloat)}, {"kept", part(1)}, {"row_status", part(2)}, {"filtered", filtered}});
@@ -305,9 +316,10 @@ PyObject* top_logits(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     v.ids = static_cast<int32_t*>(ids.data_ptr());
     v.lse = static_cast<float*>(lse.data_ptr());
     cos_status st;
-    Py_BEGIN_ALLOW_THREADS
-    st = enqueue(fn, v, logits->device().index());
-    Py_END_ALLOW_THREADS
+    {
+      const Unlocked unlocked;
+      st = enqueue(fn, v, logits->device().index());
+    }
     if (st != COS_OK) return PyLong_FromLong(st);
     return dict_of({{"values", values}, {"ids", ids}, {"lse", lse}});
   }
@@ -434,17 +446,19 @@ PyObject* distill_loss(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     at::Tensor loss;
     if (at::GradMode::is_enabled() && student->requires_grad()) {
       const std::optional<at::Tensor> lse = a[5] == Py_None ? std::optional<at::Tensor>() : THPVariable_Unpack(a[5]);  // (an undefined tensor is no argument of a node)
-      Py_BEGIN_ALLOW_THREADS
-      loss = DistillLoss::apply(*student, THPVariable_Unpack(a[3]), THPVariable_Unpack(a[4]), lse, &v, static_cast<int64_t>(fn), static_cast<int64_t>(grad_fn), &st);
-      Py_END_ALLOW_THREADS
+      {
+        const Unlocked unlocked;
+        loss = DistillLoss::apply(*student, THPVariable_Unpack(a[3]), THPVariable_Unpack(a[4]), lse, &v, static_cast<int64_t>(fn), static_cast<int64_t>(grad_fn), &st);
+      }
     } else {
       loss = floats(*student, v.rows);
       const at::Tensor statistics = floats(*student, statistics_size(v));
       v.loss = static_cast<float*>(loss.data_ptr());
       v.statistics = static_cast<float*>(statistics.data_ptr());
-      Py_BEGIN_ALLOW_THREADS
-      st = enqueue(fn, v, student->device().index());
-      Py_END_ALLOW_THREADS
+      {
+        const Unlocked unlocked;
+        st = enqueue(fn, v, student->device().index());
+      }
     }
     if (st != COS_OK) return PyLong_FromLong(st);
     return THPVariable_Wrap(loss);
@@ -473,9 +487,10 @@ PyObject* distill_step(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     v.grad = grad.data_ptr();
     v.stride_grad = v.vocab;
     cos_status st;
-    Py_BEGIN_ALLOW_THREADS
-    st = enqueue(fn, v, student->device().index());
-    Py_END_ALLOW_THREADS
+    {
+      const Unlocked unlocked;
+      st = enqueue(fn, v, student->device().index());
+    }
     if (st != COS_OK) return PyLong_FromLong(st);
     return dict_of({{"loss", loss}, {"grad", grad}});
   }

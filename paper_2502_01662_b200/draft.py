@@ -262,6 +262,7 @@ def distill_loss(student, ids, values, lse=None, weights: Optional[Sequence[floa
     is an empty entry; a token that several lists name gets the sum of its shares).  With `lse` ([rows], or [rows, lists]; the
     teachers' at the same temperature) shares are probabilities and what is not listed is left out; without, each list is
     taken to be the teacher's whole distribution.  `weights` are the ensemble's.  Differentiable in the student's logits alone, once.
+    (Lists made under torch.inference_mode() cannot be kept for a backward pass, as of any operation; made under torch.no_grad() they can.)
     A row without entries has loss 0 and gradient 0, and a row whose upstream gradient is 0 has gradient 0, whatever its logits.
     Forward and backward may be captured into a CUDA graph; of a leaf that an eager graph on the default stream still refers to,
     the backward pass is refused there."""

@@ -462,9 +462,10 @@ cos_status distill(const cos_distill_args* a, void* cuda_stream) {
   p.values = a->values;
   p.lse = a->lse;
   for (int g = 0; g < a->lists; ++g) p.w[g] = a->weights[g];
-  p.c = static_cast<float>(fmin(1.4426950408889634 / a->temperature, 3e38));
+  const Exponent exponent = exponent_of(a->temperature);
+  p.c = exponent.c;
   p.inv_T = 1.0 / a->temperature;
-  p.inv_c = p.c < 3e38f ? static_cast<double>(p.c) * 0.6931471805599453 : p.inv_T;
+  p.inv_c = exponent.value < 3e38 ? exponent.value * 0.6931471805599453 : p.inv_T;
   p.row_weights = a->row_weights;
   p.loss = a->loss;
   p.statistics = a->statistics;

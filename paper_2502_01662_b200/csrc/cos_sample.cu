@@ -1366,7 +1366,7 @@ extern "C" cos_status cos_top_logits(const cos_top_args* a, void* cuda_stream) {
   p.c.stride = a->stride_row;
   p.k = a->k;
   p.inv_T = 1.0 / a->temperature;
-  p.scale = static_cast<float>(fmin(1.4426950408889634 / a->temperature, 3e38));
+  p.scale = exponent_of(a->temperature).c;
   p.values = a->values;
   p.ids = a->ids;
   p.lse = a->lse;

@@ -9,6 +9,8 @@
 
 #include <cuda_bf16.h>
 
+#include <cfloat>
+#include <cstring>
 #include <type_traits>
 
 #include "cos_common.cuh"
@@ -392,6 +394,21 @@ inline bool overlap(const void* in, long long stride_in, const void* out, long l
   if (sa != sb) return true;
   const long long apart = ((b - a) % sa + sa) % sa;  // columns of one buffer
   return apart < row || apart > sa - row;
+}
+
+// log2(e) / T of a temperature in (0, 1e300), in 32 bits and as that number in 64.  Never 0 (at any temperature -inf is infinitely far, and 0 times it is not a number): 2^-149 from T = 2e45 on, at
+// which differences of any two logits come to less than 5e-7.  Subnormal numbers are put together from their bits, since a thread may flush them.
+struct Exponent {
+  float c;
+  double value;
+};
+inline Exponent exponent_of(double temperature) {
+  const double c = fmin(1.4426950408889634 / temperature, 3e38);
+  if (c >= FLT_MIN) return {static_cast<float>(c), static_cast<double>(static_cast<float>(c))};
+  const unsigned units = static_cast<unsigned>(fmax(c * 0x1p149 + 0.5, 1.0));
+  Exponent e = {0.0f, units * 0x1p-149};
+  memcpy(&e.c, &units, sizeof(units));
+  return e;
 }
 
 // The device of a call, made current for its duration.

@@ -5,6 +5,7 @@ Loading fails loudly if the library cannot be built or opened.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 from typing import Optional, Sequence
 
@@ -144,6 +145,20 @@ def _dtype_code(torch_dtype) -> int:
     if torch_dtype == torch.float16:
         return COS_DTYPE_F16
     raise ValueError(f"logits must be float32, bfloat16 or float16, not {torch_dtype}")
+
+
+def _memory_of(torch, stream):
+    """The context in which a call on `stream` (None: torch's current one) makes its outputs: of that stream's memory.  What the current stream's memory has free may
+    be in use by work that is queued there."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _used_here(torch, stream, device, made):
+    """Outputs made for `stream` are going to be read on the current one, which their memory waits for when they are let go."""
+    if stream is not None:
+        here = torch.cuda.current_stream(device)
+        for t in made:
+            t.record_stream(here)
 
 
 def _current_stream(torch, index: int) -> int:
@@ -301,10 +316,12 @@ class CosVerifier:
             raise ValueError("proposer must be a contiguous int32 device tensor")
         if outs is None:
             n, B, P, V = logits.shape
-            outs = self._alloc_outs(B, P, V, logits.device, diag, dump_r)
-            if lse:     # log-sum-exp behind every softmax of a position: [B, gamma+1, n] (ensemble) or [B, gamma+1, 2]
-                slots = self.cfg.n if self.cfg.combine == COS_COMBINE_PROB_ENSEMBLE else 2
-                outs["lse"] = torch.empty((B, P, slots), dtype=torch.float32, device=logits.device)
+            with _memory_of(torch, stream):
+                outs = self._alloc_outs(B, P, V, logits.device, diag, dump_r)
+                if lse:     # log-sum-exp behind every softmax of a position: [B, gamma+1, n] (ensemble) or [B, gamma+1, 2]
+                    slots = self.cfg.n if self.cfg.combine == COS_COMBINE_PROB_ENSEMBLE else 2
+                    outs["lse"] = torch.empty((B, P, slots), dtype=torch.float32, device=logits.device)
+            _used_here(torch, stream, logits.device, outs.values())
         if offset_device is not None and (offset_device.dtype != torch.int64 or not offset_device.is_cuda):
             raise ValueError("offset_device must be an int64 device tensor")
         a = self._fill_args(logits, drafts, proposer, seed, offset, row_base, flags, outs, bonus_model, offset_device)

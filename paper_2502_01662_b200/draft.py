@@ -9,7 +9,7 @@ import ctypes
 import operator
 from typing import Optional, Sequence
 
-from .binding import COS_MAX_MODELS, COS_OK, CosVerifyError, _current_stream, _dtype_code, load_call, load_library
+from .binding import COS_MAX_MODELS, COS_OK, CosVerifyError, _current_stream, _dtype_code, _memory_of, _used_here, load_call, load_library
 
 COS_TOP_MAX = 1024
 COS_DISTILL_STATISTICS = 8
@@ -105,11 +105,10 @@ def _written(torch, t):
 
 
 def _stream_of(torch, device, stream, made):
-    """The address of the stream of a call; tensors made for a stream that is not the current one stay with it."""
+    """The address of the stream of a call, whose outputs were made in its memory."""
     if stream is None:
         return _current_stream(torch, device.index)
-    for t in made:
-        t.record_stream(stream)
+    _used_here(torch, stream, device, made)
     return stream.cuda_stream
 
 
@@ -141,15 +140,17 @@ def sample(logits, uniforms, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, fil
             setattr(a, "row_" + name, _small(v, name, (rows,), dtype, device))
         else:
             setattr(a, name, v if name != "top_k" else max(-1, min(operator.index(v), 2 ** 31 - 1)))     # (a vocabulary has no more)
-    buf = torch.empty((4, rows), dtype=torch.int32, device=device)
+    with _memory_of(torch, stream):
+        buf = torch.empty((4, rows), dtype=torch.int32, device=device)
+        room = torch.empty((rows, vocab), dtype=logits.dtype, device=device) if filtered is True else None
     tokens, kept, status, prob = buf.unbind(0)
     out = {"tokens": tokens, "prob": prob.view(torch.float32), "kept": kept, "row_status": status}
     a.tokens, a.kept, a.row_status, a.prob = tokens.data_ptr(), kept.data_ptr(), status.data_ptr(), prob.data_ptr()
     made = [buf]
     if filtered is not False:
         if filtered is True:
-            filtered = torch.empty((rows, vocab), dtype=logits.dtype, device=device)
-            made.append(filtered)
+            filtered = room
+            made.append(room)
         r, v, a.stride_filtered = _rows(filtered, "filtered")
         if (r, v) != (rows, vocab) or filtered.dtype != logits.dtype or filtered.device != device:
             raise ValueError("filtered must be like the logits")
@@ -177,9 +178,10 @@ def top_logits(logits, k: int, temperature: float = 1.0, stream=None) -> dict:
     device = logits.device
     if not 1 <= k <= min(COS_TOP_MAX, vocab):
         raise ValueError(f"k must be in [1, {min(COS_TOP_MAX, vocab)}]")
-    values = torch.empty((rows, k), dtype=torch.float32, device=device)
-    ids = torch.empty((rows, k), dtype=torch.int32, device=device)
-    lse = torch.empty((rows,), dtype=torch.float32, device=device)
+    with _memory_of(torch, stream):
+        values = torch.empty((rows, k), dtype=torch.float32, device=device)
+        ids = torch.empty((rows, k), dtype=torch.int32, device=device)
+        lse = torch.empty((rows,), dtype=torch.float32, device=device)
     a = cos_top_args(logits.data_ptr(), stride, rows, vocab, _dtype_code(logits.dtype), device.index, k, temperature,
                      values.data_ptr(), ids.data_ptr(), lse.data_ptr())
     lib = _library()
@@ -211,14 +213,14 @@ def _distill_args(torch, student, ids, values, lse, weights, temperature) -> cos
     return a
 
 
-def _loss_call(student, ids, values, lse, weights, temperature, stream=None):
+def _loss_call(student, ids, values, lse, weights, temperature):
     import torch
     a = _distill_args(torch, student, ids, values, lse, weights, temperature)
     loss = torch.empty((a.rows,), dtype=torch.float32, device=student.device)
     statistics = torch.empty((a.rows * (COS_DISTILL_STATISTICS + a.lists * a.k),), dtype=torch.float32, device=student.device)
     a.loss, a.statistics = loss.data_ptr(), statistics.data_ptr()
     lib = _library()
-    _check(lib, lib.cos_distill_loss(ctypes.byref(a), _stream_of(torch, student.device, stream, (loss, statistics))))
+    _check(lib, lib.cos_distill_loss(ctypes.byref(a), _current_stream(torch, student.device.index)))
     return loss, statistics
 
 
@@ -298,16 +300,16 @@ def distill_step(student, ids, values, row_weights, lse=None, weights: Optional[
     a = _distill_args(torch, student, ids, values, lse, weights, temperature)
     device = student.device
     a.row_weights = _small(row_weights, "row_weights", (a.rows,), torch.float32, device)
-    loss = torch.empty((a.rows,), dtype=torch.float32, device=device)
-    made = [loss]
-    if grad is None:
-        grad = torch.empty((a.rows, a.vocab), dtype=student.dtype, device=device)
-        made.append(grad)
+    with _memory_of(torch, stream):
+        loss = torch.empty((a.rows,), dtype=torch.float32, device=device)
+        statistics = torch.empty((a.rows * (COS_DISTILL_STATISTICS + a.lists * a.k),), dtype=torch.float32, device=device)
+        made = [loss]
+        if grad is None:
+            grad = torch.empty((a.rows, a.vocab), dtype=student.dtype, device=device)
+            made.append(grad)
     rows, vocab, a.stride_grad = _rows(grad, "grad")
     if (rows, vocab) != (a.rows, a.vocab) or grad.dtype != student.dtype or grad.device != device:
         raise ValueError("grad must be like the student's logits")
-    statistics = torch.empty((a.rows * (COS_DISTILL_STATISTICS + a.lists * a.k),), dtype=torch.float32, device=device)
-    made.append(statistics)
     a.loss, a.statistics, a.grad = loss.data_ptr(), statistics.data_ptr(), grad.data_ptr()
     lib = _library()
     _check(lib, lib.cos_distill_step(ctypes.byref(a), _stream_of(torch, device, stream, made)))

@@ -390,6 +390,7 @@ cudaError_t launch_draw(const cos_verify_config& c, KParams& p, bool all, int sm
 }
 
 cos_status cuda_fail(cos_verify_ctx* ctx, const char* what, cudaError_t e) {
+  (void)cudaGetLastError();  // (reported here: the thread's next launch, the caller's own, must not find it)
   char buf[256];
   snprintf(buf, sizeof(buf), "%s: %s", what, cudaGetErrorString(e));
   if (ctx)

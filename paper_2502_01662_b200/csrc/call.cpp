@@ -441,7 +441,7 @@ PyObject* distill_loss(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   {
     const at::Tensor* student = nullptr;
     cos_distill_args v = {};
-    if (!distill_of(a + 2, &v, &student)) Py_RETURN_NONE;
+    if (!distill_of(a + 2, &v, &student) || student->_fw_grad(0).defined()) Py_RETURN_NONE;  // (a tangent: refused)
     cos_status st = COS_OK;
     at::Tensor loss;
     if (at::GradMode::is_enabled() && student->requires_grad()) {

@@ -263,7 +263,7 @@ def distill_loss(student, ids, values, lse=None, weights: Optional[Sequence[floa
     `ids` int32 and `values` float32 are one teacher's list [rows, k] or [rows, lists, k], as `top_logits` makes them (an id of -1
     is an empty entry; a token that several lists name gets the sum of its shares).  With `lse` ([rows], or [rows, lists]; the
     teachers' at the same temperature) shares are probabilities and what is not listed is left out; without, each list is
-    taken to be the teacher's whole distribution.  `weights` are the ensemble's.  Differentiable in the student's logits alone, once.
+    taken to be the teacher's whole distribution.  `weights` are the ensemble's.  Differentiable in the student's logits alone, once, and not in forward mode (a student with a tangent is refused).
     (Lists made under torch.inference_mode() cannot be kept for a backward pass, as of any operation; made under torch.no_grad() they can.)
     A row without entries has loss 0 and gradient 0, and a row whose upstream gradient is 0 has gradient 0, whatever its logits.
     Forward and backward may be captured into a CUDA graph; of a leaf that an eager graph on the default stream still refers to,
@@ -276,6 +276,8 @@ def distill_loss(student, ids, values, lse=None, weights: Optional[Sequence[floa
         elif got is not None:
             return got
     import torch
+    if torch.autograd.forward_ad.unpack_dual(student).tangent is not None:
+        raise NotImplementedError("distill_loss has no jvp: it is not differentiable in forward mode")
     if torch.is_grad_enabled() and student.requires_grad:
         global _distill_function
         if _distill_function is None:

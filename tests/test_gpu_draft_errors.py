@@ -108,3 +108,16 @@ def test_no_memory(way):
     flat = lambda v: list(v.values()) if isinstance(v, dict) else list(v) if isinstance(v, tuple) else [v]  # noqa: E731
     for call, before in zip(calls, want):
         assert all(torch.equal(a, b) for a, b in zip(flat(call()), flat(before)))
+
+
+def test_a_student_with_a_tangent_alone(way):
+    """No gradient is wanted, and none may be lost: neither in a graph nor without one."""
+    s, ids, values, lse, _ = make()
+    want = pkg.distill_loss(s, ids, values, lse)
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(s, torch.ones_like(s))
+        for grad in (True, False):
+            with torch.set_grad_enabled(grad), pytest.raises(NotImplementedError, match="forward mode"):
+                pkg.distill_loss(dual, ids, values, lse)
+        assert torch.equal(pkg.distill_loss(forward_ad.unpack_dual(dual).primal, ids, values, lse), want)
+    assert torch.equal(pkg.distill_loss(s, ids, values, lse), want)

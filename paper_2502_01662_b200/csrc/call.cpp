@@ -371,6 +371,14 @@ void refuse_capture(const at::Tensor& student) {
   TORCH_CHECK(!on || on->id() != 0, "distill_loss: a backward pass of this leaf cannot be captured while an eager graph of it is alive");
 }
 
+// refuse_capture(student): raises where that is so, for the autograd function of the long way.
+PyObject* refuse_capture(PyObject*, PyObject* o) {
+  HANDLE_TH_ERRORS
+  if (THPVariable_Check(o)) refuse_capture(THPVariable_Unpack(o));
+  Py_RETURN_NONE;
+  END_HANDLE_TH_ERRORS
+}
+
 // The loss as a node of the autograd graph.  `grad_fn` is cos_distill_grad; `st` takes the status of the forward call.
 struct DistillLoss : torch::autograd::Function<DistillLoss> {
   static at::Tensor forward(torch::autograd::AutogradContext* ctx, const at::Tensor& student, const at::Tensor& ids, const at::Tensor& values, const std::optional<at::Tensor>& lse, const cos_distill_args* args,
@@ -506,6 +514,7 @@ PyMethodDef methods[] = {{"callee", callee, METH_VARARGS, "a context, for run"},
                          {"top_logits", fast(top_logits), METH_FASTCALL, "one call of cos_top_logits"},
                          {"distill_loss", fast(distill_loss), METH_FASTCALL, "one call of cos_distill_loss, with its gradient"},
                          {"distill_step", fast(distill_step), METH_FASTCALL, "one call of cos_distill_step"},
+                         {"refuse_capture", static_cast<PyCFunction>(refuse_capture), METH_O, "an error where a backward pass of this leaf must not be captured"},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -224,6 +224,16 @@ def _loss_call(student, ids, values, lse, weights, temperature):
     return loss, statistics
 
 
+def _refuse_capture(torch, student):
+    """A captured backward pass of a leaf whose eager graph is alive would end the process.  Whether one is can be seen in native code alone; without that none is captured."""
+    if not student.requires_grad or not student.is_leaf or not torch.cuda.is_current_stream_capturing():
+        return
+    native = _calls()
+    if not native:
+        raise RuntimeError("distill_loss: a backward pass of a leaf cannot be captured without the module of csrc/call.cpp (an eager graph of it may be alive)")
+    native[0].refuse_capture(student)
+
+
 def _function():
     """The autograd function, made on first use (the module does not import torch)."""
     import torch
@@ -241,6 +251,7 @@ def _function():
         @once_differentiable
         def backward(ctx, upstream):
             student, ids, values, lse, statistics = ctx.saved_tensors
+            _refuse_capture(torch, student)
             a = _distill_args(torch, student, ids, values, lse, ctx.weights, ctx.temperature)
             upstream = upstream.contiguous()    # (an expanded scalar, of a mean or a sum)
             grad = torch.empty((a.rows, a.vocab), dtype=student.dtype, device=student.device)
@@ -267,7 +278,8 @@ def distill_loss(student, ids, values, lse=None, weights: Optional[Sequence[floa
     (Lists made under torch.inference_mode() cannot be kept for a backward pass, as of any operation; made under torch.no_grad() they can.)
     A row without entries has loss 0 and gradient 0, and a row whose upstream gradient is 0 has gradient 0, whatever its logits.
     Forward and backward may be captured into a CUDA graph; of a leaf that an eager graph on the default stream still refers to,
-    the backward pass is refused there."""
+    the backward pass is refused there (of any leaf, where csrc/call.cpp cannot be built).  The leaves behind a student that is computed are not looked at: no eager graph of theirs
+    may be alive."""
     native = _calls()
     if native:
         got = native[0].distill_loss(native[3], native[4], student, ids, values, lse, weights, temperature)

@@ -95,7 +95,7 @@ class AlternateProposal:
         self.verify_seed = verify_seed
         self._u = np.random.Generator(np.random.Philox(key=propose_seed))
         self.keep_history = keep_history
-        self.propose = _checked(propose, self.T)
+        self.propose = _checked(propose, self.T, verify, models[0].vocab)
 
     # Propose: one token from model i after `prefix`, at the temperature of the run
     def _propose_one(self, i: int, prefix: Sequence[int]) -> int:
@@ -186,7 +186,7 @@ class CollaborativeSpeculation:
         self.keep_events = keep_events
         self.events: List[Event] = []
         self.calls = 0         # verification calls so far: the counter offset of the next one
-        self.propose = _checked(propose, self.T)
+        self.propose = _checked(propose, self.T, verify, models[0].vocab)
 
     def _log(self, *a):
         if self.keep_events:
@@ -272,9 +272,15 @@ class CollaborativeSpeculation:
         return S[start:], st
 
 
-def _checked(propose, temperature: float):
-    if propose is not None and propose.temperature != temperature:
+def _checked(propose, temperature: float, verify, vocab: int):
+    """A proposer that a run can take: of its temperature, and, where the run combines logits, one that leaves every token its logit (a combination of -inf is not a number, and models that
+    keep different tokens may leave none).  `verify` says which run that is by its attribute logit_linear, the proposer what it leaves by its method rules_out; neither has to."""
+    if propose is None:
+        return None
+    if propose.temperature != temperature:
         raise ValueError("the proposer's temperature is not the run's")
+    if getattr(verify, "logit_linear", False) and getattr(propose, "rules_out", lambda vocab: False)(vocab):
+        raise ValueError("a logit-linear run takes no limits, and greedily no proposer (without one it draws the same tokens)")
     return propose
 
 
@@ -288,7 +294,7 @@ class GpuProposer:
 
     `draw` gives a token of one row; `law` the rows with -inf at every token that could not have been drawn, which
     is what the verification has to take as the models' logits.  (Ruled-out tokens have a meaning in an ensemble; a
-    logit-linear combination of -inf is not a number, and such a run takes no limits.)"""
+    logit-linear combination of -inf is not a number, and the schedulers refuse such a run where anything is ruled out.)"""
 
     def __init__(self, temperature: float, top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0, device: int = 0):
         self.temperature = float(temperature)
@@ -300,6 +306,11 @@ class GpuProposer:
         from .draft import sample
         logits = torch.from_numpy(np.ascontiguousarray(rows, dtype=np.float32)).to(self._device)
         return sample(logits, torch.from_numpy(uniforms.astype(np.float32)).to(self._device), *self._limits, filtered=filtered)
+
+    def rules_out(self, vocab: int) -> bool:
+        """Whether `law` may leave a token of a vocabulary of that size without its logit."""
+        temperature, top_k, top_p, min_p = self._limits
+        return temperature == 0.0 or 0 < top_k < vocab or top_p < 1.0 or min_p > 0.0
 
     def draw(self, row: np.ndarray, uniform: float) -> int:
         return int(self._sample(row.reshape(1, -1), np.array([uniform]), False)["tokens"][0])
@@ -314,7 +325,7 @@ def gpu_verify(combine: int, weights: Sequence[float], temperature: float, vocab
     """The verification call of the CUDA library for the schedulers: one context per proposal length,
     made on first use, host tensors in and out (cos_verify_run_host)."""
     import torch
-    from .binding import CosVerifier
+    from .binding import COS_COMBINE_LOGIT_LINEAR, CosVerifier
     ctxs = {}
     n = len(list(weights))
 
@@ -329,5 +340,6 @@ def gpu_verify(combine: int, weights: Sequence[float], temperature: float, vocab
                                 prop, seed, offset, bonus_model=bonus_model)
         return int(outs["accept_count"][0]), outs["out_tokens"][0].numpy().copy(), float(outs["bonus_prob"][0])
 
+    verify.logit_linear = combine == COS_COMBINE_LOGIT_LINEAR
     verify.close = lambda: [c.close() for c in ctxs.values()]
     return verify

@@ -102,7 +102,7 @@ class AlternateProposal:
         m = self.models[i]
         m.calls += 1
         if self.propose is not None:
-            return self.propose.draw(m.logits(prefix), self._u.random())
+            return _token(self.propose.draw(m.logits(prefix), self._u.random()))
         l = m.logits(prefix).astype(np.float64)
         if self.T == 0.0:
             return int(np.argmax(l))
@@ -140,8 +140,8 @@ class AlternateProposal:
             logits = _laws(self.propose, logits)
             drafts = np.asarray(T, dtype=np.int32).reshape(1, g)
             a, out, prob = self.verify(logits, drafts, proposer, verifier, self.verify_seed, st.cycles)
-            emitted = [int(x) for x in out[: a + 1]] if a < g else [int(x) for x in out[:g]]
-            bonus = int(out[g]) if a == g else None
+            emitted = [_token(x) for x in out[: a + 1]] if a < g else [_token(x) for x in out[:g]]
+            bonus = _token(out[g]) if a == g else None
             if self.keep_history:
                 st.history.append(CycleRecord(proposer, len(C), list(T), int(a), emitted, bonus))
             S += emitted
@@ -196,7 +196,7 @@ class CollaborativeSpeculation:
         m = self.models[i]
         m.calls += 1
         if self.propose is not None:
-            return self.propose.draw(m.logits(prefix), self._u.random())
+            return _token(self.propose.draw(m.logits(prefix), self._u.random()))
         l = m.logits(prefix).astype(np.float64)
         if self.T == 0.0:
             return int(np.argmax(l))
@@ -236,7 +236,7 @@ class CollaborativeSpeculation:
             lg = np.broadcast_to(row, (n, 1, 1, V)).astype(np.float32).copy()
             _, out, prob = self.verify(lg, np.zeros((1, 0), np.int32), 0, i, self.verify_seed, self.calls)
             self.calls += 1
-            Sc.append(int(out[0]))
+            Sc.append(_token(out[0]))
             owner.append(i)
             scored[i] = len(Sc)
             # Verify every cached token that all models have scored
@@ -261,7 +261,7 @@ class CollaborativeSpeculation:
                     scored = [c - L for c in scored]
                     st.full_accepts += 1
                 else:
-                    S += Sc[:a] + [int(out[a])]           # the resampled token replaces the rejected one
+                    S += Sc[:a] + [_token(out[a])]           # the resampled token replaces the rejected one
                     Sc.clear()
                     owner.clear()
                     scored = [0] * n
@@ -282,6 +282,13 @@ def _checked(propose, temperature: float, verify, vocab: int):
     if getattr(verify, "logit_linear", False) and getattr(propose, "rules_out", lambda vocab: False)(vocab):
         raise ValueError("a logit-linear run takes no limits, and greedily no proposer (without one it draws the same tokens)")
     return propose
+
+
+def _token(x) -> int:
+    """A token that a proposer or a verification answered with; -1 is none: its row of logits holds no distribution."""
+    if x < 0:
+        raise ValueError("no token: a row of logits holds a NaN or +inf, or nothing but -inf")
+    return int(x)
 
 
 def _laws(propose, logits: np.ndarray) -> np.ndarray:

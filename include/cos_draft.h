@@ -118,7 +118,9 @@ typedef struct {
  * Distillation of a student (the proposer) from the largest logits of its teachers (the models its drafts are verified against).  With the
  * target t(x) = sum_g w_g p_g(x) over the listed tokens, p_g(x) = exp(v(x) / T - lse_g), and q = softmax(s / T):
  *   loss = sum_x t(x) (ln t(x) - ln q(x)),   gradient = row_weight / T * (P q(x) - t(x)),  P = sum_x t(x).
- * +inf where a token with a share has the logit -inf.  A row without a share (padding) has loss 0 and gradient 0 and is not read.
+ * +inf where a token with a share has the logit -inf.  A row without a share (padding) has loss 0 and gradient 0 whatever its logits are; the first rows of a call may be read
+ * before that is known, so `student` has to hold all of them.  A teacher whose row holds a NaN or +inf lists nothing (cos_top_logits) and counts as one that is absent: its share of the
+ * target is missing, or the row is padding where no other teacher lists anything.  Its lse tells it, which is not looked at here where no entry refers to it.
  *   cos_distill_loss  loss and statistics (row_weights, grad are not looked at)
  *   cos_distill_grad  the gradient, from the statistics of the same student, lists and T (loss is not looked at)
  *   cos_distill_step  loss and gradient, reading the student once

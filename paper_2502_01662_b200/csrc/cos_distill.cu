@@ -9,7 +9,8 @@
 // launch with both stay in the shared memory of a cluster of blocks between the normaliser and the gradient, and are read once.  Three blocks of a multiprocessor
 // have up to 64 KB each under way, since a row's chain of steps (copies, two sweeps, a barrier, the gradient) takes longer than its bytes.
 // Measured: loss of 1024 x 128256 bf16 48 us (5.0 TB/s of what is not padding), its gradient 78 (6.4); both of 2048 x 32000 bf16 59 us, 4.0 TB/s, with the issue slots 68 % busy; both of
-// 100 x 50001 fp32 14.4 us, of which the shares are 3.
+// 100 x 50001 fp32 14.4 us, of which the shares are 3.  The shares compare every entry of a row with all of them, which is next to nothing for 64 entries and most of the time for many: both of 2048 x 32000
+// bf16 without padding 64 us with 64 entries, 116 with 256, 274 with 512, 900 with 1024.
 // Exponentials are 32-bit (2^-22) and sums of them 64-bit; shares, logarithms and the loss are 64-bit; the gradient is rounded once.
 #include "cos_slice.cuh"
 

@@ -1247,6 +1247,9 @@ cos_status check_rows(const void* logits, long long stride, int rows, int vocab,
 //   a draw, k <= 64         16   64 of 16 x 128256 bf16 11.5 / 11.0, of 8 x 256000 (k = 50) 11.8 / 12.1, of 100 x 128256 26.5 / 11.7
 //   a draw, more            40   200 of 40 x 128256 bf16 22.3 / 20.2, of 32 rows 19.7 / 20.7, of 100 33.9 / 20.9
 //   the largest logit       16   16 x 128256 bf16 5.0 / 4.6, 100 rows 13.2 / 4.8, 64 x 32000 4.7 / 3.3; not for shorter rows (256 x 16000 4.2 / 5.2)
+// Rows whose limit lies among so many equal logits that the list does not hold them are swept again from memory, which a block alone does longer than a cluster (128256 bf16, a row of three values, one row less /
+// as many rows: a draw of 64 at 16 rows 40 / 229, of 200 at 40 rows 101 / 232, top 64 at 48 rows 54 / 144, top 288 at 80 rows 84 / 149; bf16 of uniform numbers, a few dozen of each value: 12 / 20, 67 / 160, 16 / 23,
+// 112 / 200).  The host cannot see it, and logits of models are not like that.
 bool own_blocks(int rows, int vocab, int dtype, int from, int longer_than = kMostKept) { return rows >= from && static_cast<long long>(vocab) * (dtype == COS_DTYPE_F32 ? 4 : 2) > longer_than; }
 
 template <class P, class F>

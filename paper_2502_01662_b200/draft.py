@@ -165,7 +165,8 @@ def sample(logits, uniforms, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, fil
 
 def top_logits(logits, k: int, temperature: float = 1.0, stream=None) -> dict:
     """cos_top_logits: "values" (float32) and "ids" (int32), [rows, k], of the k largest logits of each row, the largest first,
-    and "lse" [rows] float32, ln sum_x exp(l(x) / temperature): what `distill_loss` takes of a teacher."""
+    and "lse" [rows] float32, ln sum_x exp(l(x) / temperature): what `distill_loss` takes of a teacher.  A row with a NaN or +inf lists
+    nothing (ids -1) and has a NaN for "lse".  The outputs carry no gradient."""
     native = _calls() if stream is None else None
     if native:
         got = native[0].top_logits(native[2], logits, k, temperature)
@@ -276,7 +277,7 @@ def distill_loss(student, ids, values, lse=None, weights: Optional[Sequence[floa
     teachers' at the same temperature) shares are probabilities and what is not listed is left out; without, each list is
     taken to be the teacher's whole distribution.  `weights` are the ensemble's.  Differentiable in the student's logits alone, once, and not in forward mode (a student with a tangent is refused).
     (Lists made under torch.inference_mode() cannot be kept for a backward pass, as of any operation; made under torch.no_grad() they can.)
-    A row without entries has loss 0 and gradient 0, and a row whose upstream gradient is 0 has gradient 0, whatever its logits.
+    A row without entries has loss 0 and gradient 0 (so has one whose only teacher held a NaN there, and one teacher of several that did is left out: "lse" is NaN then), and a row whose upstream gradient is 0 has gradient 0, whatever its logits.
     Forward and backward may be captured into a CUDA graph; of a leaf that an eager graph on the default stream still refers to,
     the backward pass is refused there (of any leaf, where csrc/call.cpp cannot be built).  The leaves behind a student that is computed are not looked at: no eager graph of theirs
     may be alive."""
